@@ -4,7 +4,8 @@
  * One library, two compute entry points: flashrnn_fwd runs the strictly sequential, head-wise
  * block-diagonal recurrence for all T steps in one persistent kernel (bf16 calls of one step, but for
  * many rows or heads, on a kernel of their own), flashrnn_bwd runs back-propagation through time and the
- * weight-gradient reduction.
+ * weight-gradient reduction.  Beside them, what a language model does around its recurrent layers: embedding, layer norm,
+ * cross entropy, clipping by the global gradient norm (flashrnn_embedding_*, _layer_norm_*, _cross_entropy, _grad_clip).
  *
  * Conventions for every function below
  *   - All tensor pointers are DEVICE pointers owned by the caller; the library never allocates or
@@ -223,6 +224,104 @@ int flashrnn_profile_kernel_ms(int backward, float* mean_ms, int* launches);
  */
 int flashrnn_trace_phases(const flashrnn_desc_t* desc, const void* workspace, int backward, double* clocks, int* waves,
                           void* hip_stream);
+
+/*
+ * Around the time-step loop: what a language model does before and after its recurrent layers.  The conventions at the top hold (device
+ * pointers, one stream, no allocation, kernel launches only, nothing kept between calls); tensors may be empty (0 tokens or rows), pointers need
+ * the alignment of their element only, and offsets are 64-bit.  io types are flashrnn_dtype_t, index types:
+ */
+typedef enum { FLASHRNN_I32 = 2, FLASHRNN_I64 = 3 } flashrnn_index_t;
+
+/*
+ * Embedding lookup:  out[i] = scale * table[token_i],  i = 0..tokens-1.  A token outside [0, vocab) (padding, say -1) gives a row of zeros
+ * and has no gradient.
+ *   table   [vocab,width]  table_dtype
+ *   tokens  [tokens]       index_dtype
+ *   out     [tokens,width] io_dtype
+ * Gradient:  dtable[v] = scale * sum over the places i of word v of dout[i],  each sum in the order of the places (the tokens are sorted
+ * first): the result does not depend on how the workgroups run.
+ *   dout    [tokens,width] io_dtype
+ *   dtable  [vocab,width]  f32      OUT: every row, zeros for words that do not occur; accumulate != 0: the sums are added to what is there and
+ *                                   other rows are not touched (weights tied to an output layer)
+ *   workspace  flashrnn_embedding_workspace_bytes() bytes, 256-byte aligned, any content (gradient only)
+ */
+typedef struct {
+    long long tokens;   /* >= 0, below 2^31 for the gradient */
+    int vocab, width;   /* > 0 */
+    int table_dtype, io_dtype, index_dtype;
+    float scale;
+} flashrnn_embedding_desc_t;
+
+size_t flashrnn_embedding_workspace_bytes(const flashrnn_embedding_desc_t* desc);
+int flashrnn_embedding_fwd(const flashrnn_embedding_desc_t* desc, const void* table, const void* tokens, void* out, void* hip_stream);
+int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* desc, const void* tokens, const void* dout, void* dtable, int accumulate, void* workspace, void* hip_stream);
+
+/*
+ * Layer norm of every row of `width` values:  mean = E x,  rstd = 1 / sqrt(E (x - mean)^2 + eps),  y = (x - mean) rstd weight + bias.
+ * `groups` consecutive rows have a weight row each (1: one for all; NH: head by head), and x may lie inside a larger tensor: row
+ * ((o * rows_inner + i) * groups + g) of the problem starts at element o * x_stride + (i * groups + g) * width of x.  The hidden states of a
+ * flashrnn_fwd call are the rows of states + S*B*NH*D with rows_outer = T, rows_inner = B, groups = NH, x_stride = S*B*NH*D.
+ *   x        x_dtype, as above
+ *   weight, bias  [groups,width] param_dtype, each may be NULL (ones, zeros)
+ *   y        [rows,width] io_dtype  OUT
+ *   mean, rstd  [rows] f32          OUT, both NULL for a call that saves nothing (rows = rows_outer * rows_inner * groups)
+ * Gradient:  g = dy weight,  xh = (x - mean) rstd,  dx = rstd (g - E g - xh E(g xh)),  dweight = sum_rows dy xh,  dbias = sum_rows dy, the
+ * two sums in an order that the shape alone decides.
+ *   dy       [rows,width] io_dtype
+ *   dx       [rows,width] dx_dtype  OUT (dense)
+ *   dweight, dbias  [groups,width] f32  OUT, each may be NULL
+ *   workspace  flashrnn_layer_norm_workspace_bytes() bytes, 256-byte aligned, any content (may be NULL where both sums are)
+ */
+typedef struct {
+    long long rows_outer, rows_inner, x_stride;   /* >= 0 */
+    int groups, width;                            /* > 0 */
+    int x_dtype, io_dtype, dx_dtype, param_dtype;
+    float eps;                                    /* >= 0 */
+} flashrnn_layer_norm_desc_t;
+
+size_t flashrnn_layer_norm_workspace_bytes(const flashrnn_layer_norm_desc_t* desc);
+int flashrnn_layer_norm_fwd(const flashrnn_layer_norm_desc_t* desc, const void* x, const void* weight, const void* bias, void* y, void* mean, void* rstd, void* hip_stream);
+int flashrnn_layer_norm_bwd(const flashrnn_layer_norm_desc_t* desc, const void* dy, const void* x, const void* weight, const void* mean, const void* rstd,
+                            void* dx, void* dweight, void* dbias, void* workspace, void* hip_stream);
+
+/*
+ * Cross entropy of rows of logits against one class each, and its gradient in the same pass:
+ *     lse = log sum_j exp x_j,   loss = lse - x_target,   dx_j = grad_scale * dloss * (exp(x_j - lse) - [j = target])
+ * A target outside [0, classes) is ignored: its loss is 0 and so is its row of the gradient.  Classes whose logit is -inf take no part; a row of
+ * nothing else has loss +inf and gradient 0.
+ *   logits   [rows,classes] io_dtype, rows logits_stride elements apart
+ *   targets  [rows]         index_dtype
+ *   dloss    [rows] f32     gradient of every row's loss, or NULL for ones
+ *   loss     [rows] f32     OUT
+ *   lse      [rows] f32     OUT, or NULL
+ *   dlogits  [rows,classes] io_dtype, rows dlogits_stride elements apart  OUT, or NULL for the loss alone; may be `logits` itself (same stride)
+ */
+typedef struct {
+    long long rows, logits_stride, dlogits_stride;   /* rows >= 0, strides >= classes */
+    int classes;                                     /* > 0 */
+    int io_dtype, index_dtype;
+    float grad_scale;
+} flashrnn_cross_entropy_desc_t;
+
+int flashrnn_cross_entropy(const flashrnn_cross_entropy_desc_t* desc, const void* logits, const void* targets, const void* dloss, void* loss, void* lse, void* dlogits,
+                           void* hip_stream);
+
+/*
+ * Clipping by the global norm:  norm = sqrt(sum of the squares of all values of all tensors),  factor = 1 where norm <= max_norm, else
+ * max_norm / norm,  out_k = factor * grad_k.  The squares are added in 64 bits, in a fixed order.  A NaN or an infinity in any tensor makes the norm NaN or infinite
+ * and goes through the same formula (NaN: every value becomes NaN).
+ *   count       number of tensors
+ *   grads, out  HOST arrays of `count` device pointers; out[k] may be grads[k] (in place: nothing is written where the factor is 1), and out may be
+ *               NULL (the norm alone); any other overlap is undefined
+ *   sizes       HOST array: values per tensor, >= 0
+ *   dtypes      HOST array: flashrnn_dtype_t of grads[k] and out[k]
+ *   norm        [1] f32  OUT
+ *   workspace   flashrnn_grad_clip_workspace_bytes(count) bytes, 256-byte aligned, any content
+ * The host arrays are read before the call returns.
+ */
+size_t flashrnn_grad_clip_workspace_bytes(int count);
+int flashrnn_grad_clip(int count, const void* const* grads, void* const* out, const long long* sizes, const int* dtypes, float max_norm, void* norm, void* workspace,
+                       void* hip_stream);
 
 const char* flashrnn_status_string(int status);
 

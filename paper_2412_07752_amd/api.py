@@ -16,6 +16,7 @@ from .build import binding_stamp
 
 FLASHRNN_LSTM, FLASHRNN_GRU, FLASHRNN_SLSTM, FLASHRNN_ELMAN, FLASHRNN_GRU4 = 0, 1, 2, 3, 4
 FLASHRNN_F32, FLASHRNN_BF16 = 0, 1
+FLASHRNN_I32, FLASHRNN_I64 = 2, 3
 FLASHRNN_OK = 0
 FLASHRNN_ERR_NULL, FLASHRNN_ERR_SHAPE, FLASHRNN_ERR_UNSUPPORTED = -1, -2, -3
 FLASHRNN_ERR_WORKSPACE, FLASHRNN_ERR_LAUNCH, FLASHRNN_ERR_TIMEOUT, FLASHRNN_ERR_SCRATCH = -4, -5, -6, -7
@@ -32,6 +33,21 @@ _native = None   # the native module, bound to the loaded library
 class flashrnn_desc_t(ctypes.Structure):
     _fields_ = [("cell", ctypes.c_int), ("T", ctypes.c_int), ("B", ctypes.c_int), ("NH", ctypes.c_int), ("D", ctypes.c_int),
                 ("io_dtype", ctypes.c_int), ("recurrent_grad_clip", ctypes.c_float)]
+
+
+class flashrnn_embedding_desc_t(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_longlong), ("vocab", ctypes.c_int), ("width", ctypes.c_int), ("table_dtype", ctypes.c_int), ("io_dtype", ctypes.c_int),
+                ("index_dtype", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+class flashrnn_layer_norm_desc_t(ctypes.Structure):
+    _fields_ = [("rows_outer", ctypes.c_longlong), ("rows_inner", ctypes.c_longlong), ("x_stride", ctypes.c_longlong), ("groups", ctypes.c_int), ("width", ctypes.c_int),
+                ("x_dtype", ctypes.c_int), ("io_dtype", ctypes.c_int), ("dx_dtype", ctypes.c_int), ("param_dtype", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class flashrnn_cross_entropy_desc_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_longlong), ("logits_stride", ctypes.c_longlong), ("dlogits_stride", ctypes.c_longlong), ("classes", ctypes.c_int), ("io_dtype", ctypes.c_int),
+                ("index_dtype", ctypes.c_int), ("grad_scale", ctypes.c_float)]
 
 
 class FlashRNNError(RuntimeError):
@@ -99,6 +115,25 @@ def lib():
         L.flashrnn_profile_kernel_ms.restype = ctypes.c_int
         L.flashrnn_trace_phases.argtypes = [dp, vp, ctypes.c_int, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int), vp]
         L.flashrnn_trace_phases.restype = ctypes.c_int
+        ep, np_, cp = (ctypes.POINTER(t) for t in (flashrnn_embedding_desc_t, flashrnn_layer_norm_desc_t, flashrnn_cross_entropy_desc_t))
+        L.flashrnn_embedding_workspace_bytes.argtypes = [ep]
+        L.flashrnn_embedding_workspace_bytes.restype = ctypes.c_size_t
+        L.flashrnn_embedding_fwd.argtypes = [ep] + [vp] * 4
+        L.flashrnn_embedding_fwd.restype = ctypes.c_int
+        L.flashrnn_embedding_bwd.argtypes = [ep] + [vp] * 3 + [ctypes.c_int] + [vp] * 2
+        L.flashrnn_embedding_bwd.restype = ctypes.c_int
+        L.flashrnn_layer_norm_workspace_bytes.argtypes = [np_]
+        L.flashrnn_layer_norm_workspace_bytes.restype = ctypes.c_size_t
+        L.flashrnn_layer_norm_fwd.argtypes = [np_] + [vp] * 7
+        L.flashrnn_layer_norm_fwd.restype = ctypes.c_int
+        L.flashrnn_layer_norm_bwd.argtypes = [np_] + [vp] * 10
+        L.flashrnn_layer_norm_bwd.restype = ctypes.c_int
+        L.flashrnn_cross_entropy.argtypes = [cp] + [vp] * 7
+        L.flashrnn_cross_entropy.restype = ctypes.c_int
+        L.flashrnn_grad_clip_workspace_bytes.argtypes = [ctypes.c_int]
+        L.flashrnn_grad_clip_workspace_bytes.restype = ctypes.c_size_t
+        L.flashrnn_grad_clip.argtypes = [ctypes.c_int, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp]
+        L.flashrnn_grad_clip.restype = ctypes.c_int
         L.flashrnn_status_string.argtypes = [ctypes.c_int]
         L.flashrnn_status_string.restype = ctypes.c_char_p
         native = _load_native()
@@ -110,7 +145,8 @@ def lib():
 
 EXPORTS = ["flashrnn_num_states", "flashrnn_num_gates", "flashrnn_gate_cache_bytes", "flashrnn_workspace_bytes", "flashrnn_fwd",
            "flashrnn_fwd_static_scratch", "flashrnn_bwd", "flashrnn_bwd_recompute", "flashrnn_recompute_workspace_bytes", "flashrnn_check", "flashrnn_plan", "flashrnn_plan_kernel", "flashrnn_profile_enable", "flashrnn_profile_kernel_ms",
-           "flashrnn_trace_phases", "flashrnn_status_string"]
+           "flashrnn_trace_phases", "flashrnn_status_string", "flashrnn_embedding_workspace_bytes", "flashrnn_embedding_fwd", "flashrnn_embedding_bwd", "flashrnn_layer_norm_workspace_bytes",
+           "flashrnn_layer_norm_fwd", "flashrnn_layer_norm_bwd", "flashrnn_cross_entropy", "flashrnn_grad_clip_workspace_bytes", "flashrnn_grad_clip"]
 
 
 def status_string(status):
@@ -372,3 +408,225 @@ def flashrnn_check(desc, workspace, stream=None):
     rc = lib().flashrnn_check(ctypes.byref(desc), ws, _stream(stream))
     if rc != FLASHRNN_OK:
         raise FlashRNNError(rc, "flashrnn_check")
+
+
+# ---- around the time-step loop -------------------------------------------------------------------------------------------------------------
+def _index_dtype(t):
+    if t.dtype == torch.int64:
+        return FLASHRNN_I64
+    if t.dtype == torch.int32:
+        return FLASHRNN_I32
+    raise TypeError(f"tokens and targets must be int64 or int32, got {t.dtype}")
+
+
+def _same_device(first, **others):
+    for name, t in others.items():
+        if t is not None and t.device != first.device:
+            raise ValueError(f"{name} is on {t.device}, the other tensors on {first.device}")
+
+
+def _sized_workspace(workspace, n, device):
+    """The caller's workspace if it holds n bytes, a new one if there is none."""
+    if workspace is None:
+        return torch.empty(n, dtype=torch.uint8, device=device)
+    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < n:
+        raise ValueError(f"workspace must be a contiguous device tensor of at least {n} bytes")
+    return workspace
+
+
+def flashrnn_embedding_workspace_bytes(tokens, vocab, width=1):
+    """Bytes of workspace of the gradient for this many tokens."""
+    d = flashrnn_embedding_desc_t(int(tokens), int(vocab), int(width), FLASHRNN_F32, FLASHRNN_F32, FLASHRNN_I64, 1.0)
+    return lib().flashrnn_embedding_workspace_bytes(ctypes.byref(d))
+
+
+def flashrnn_embedding_fwd(table, tokens, scale=1.0, dtype=None, out=None, stream=None):
+    """out[..., :] = scale * table[tokens[...], :], in the table's type or in `dtype`.  table[vocab, width] bf16 or f32, tokens of any shape, int64 or int32;
+    tokens outside the vocabulary give zeros."""
+    V, H = table.shape
+    dtype = (table.dtype if dtype is None else dtype) if out is None else out.dtype
+    _chk(table, (V, H), table.dtype, "table")
+    _chk(tokens, tokens.shape, tokens.dtype, "tokens")
+    if out is None:
+        out = torch.empty((*tokens.shape, H), dtype=dtype, device=table.device)
+    _chk(out, (*tokens.shape, H), dtype, "out")
+    _same_device(table, tokens=tokens, out=out)
+    d = flashrnn_embedding_desc_t(tokens.numel(), V, H, _io_dtype(table), _io_dtype(out), _index_dtype(tokens), float(scale))
+    rc = lib().flashrnn_embedding_fwd(ctypes.byref(d), _ptr(table), _ptr(tokens), _ptr(out), _stream(stream))
+    if rc != FLASHRNN_OK:
+        raise FlashRNNError(rc, "flashrnn_embedding_fwd")
+    return out
+
+
+def flashrnn_embedding_bwd(tokens, dout, vocab, scale=1.0, dtable=None, accumulate=False, workspace=None, stream=None):
+    """dtable[v] = scale * sum of dout over the places of word v; dtable[vocab, width] f32.  accumulate: added to the dtable passed in, rows of words that do not
+    occur untouched.  The same result on every run."""
+    H = dout.shape[-1]
+    _chk(dout, (*tokens.shape, H), dout.dtype, "dout")
+    _chk(tokens, tokens.shape, tokens.dtype, "tokens")
+    if dtable is None:
+        if accumulate:
+            raise ValueError("dtable is required to accumulate into")
+        dtable = torch.empty((int(vocab), H), dtype=torch.float32, device=dout.device)
+    _chk(dtable, (int(vocab), H), torch.float32, "dtable")
+    _same_device(dout, tokens=tokens, dtable=dtable, workspace=workspace)
+    d = flashrnn_embedding_desc_t(tokens.numel(), int(vocab), H, FLASHRNN_F32, _io_dtype(dout), _index_dtype(tokens), float(scale))
+    n = lib().flashrnn_embedding_workspace_bytes(ctypes.byref(d))
+    workspace = _sized_workspace(workspace, n, dout.device)
+    rc = lib().flashrnn_embedding_bwd(ctypes.byref(d), _ptr(tokens), _ptr(dout), _ptr(dtable), int(bool(accumulate)), _ptr(workspace), _stream(stream))
+    if rc != FLASHRNN_OK:
+        raise FlashRNNError(rc, "flashrnn_embedding_bwd")
+    return dtable
+
+
+def _rows_of(x, inner):
+    """(outer, inner, stride): x's leading axes as `outer` blocks of dense rows, `stride` elements apart; `inner` trailing axes are a row."""
+    width = 1
+    for n, step in zip(reversed(x.shape[-inner:]), reversed(x.stride()[-inner:])):
+        if n != 1 and step != width:
+            raise ValueError("the rows of x must be dense")
+        width *= n
+    outer, dense, stride, first = 1, 1, 0, True   # (from the last axis: dense so far, then one strided axis, then nothing but its continuation)
+    for n, step in zip(reversed(x.shape[:-inner]), reversed(x.stride()[:-inner])):
+        if n == 1:
+            continue
+        if first and step == dense * width:
+            dense *= n
+        elif first:
+            outer, stride, first = n, step, False
+        elif step == stride * outer:
+            outer *= n
+        else:
+            raise ValueError("x must be dense but for one of its leading axes")
+    return (0, 0, 0) if x.numel() == 0 else (outer, dense, stride)
+
+
+def _norm_desc(x, weight, bias, io, dx, eps):
+    if not x.is_cuda:
+        raise ValueError("x must be a device tensor")
+    params = weight if weight is not None else bias
+    if params is None:
+        groups, width, shape = 1, x.shape[-1], None
+    else:
+        shape = tuple(params.shape)
+        if len(shape) not in (1, 2) or tuple(x.shape[-len(shape):]) != shape:
+            raise ValueError(f"weight and bias are [D] or [NH, D], the last axes of x: got {shape} for x {tuple(x.shape)}")
+        groups, width = (1, *shape)[-2:]
+        for t, name in ((weight, "weight"), (bias, "bias")):
+            _chk(t, shape, params.dtype, name, optional=True)
+    outer, inner, stride = _rows_of(x, 1 if shape is None else len(shape))
+    return flashrnn_layer_norm_desc_t(outer, inner, stride, groups, width, _io_dtype(x), _io_dtype(io), _io_dtype(dx), FLASHRNN_F32 if params is None else _io_dtype(params), float(eps))
+
+
+def flashrnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, dtype=None, save_for_backward=True, y=None, mean=None, rstd=None, stream=None):
+    """Layer norm over the last axis of x, in x's type or in `dtype`.  weight, bias: [D], or [NH, D] for x[..., NH, D] (head by head), or None.  x may have one leading
+    axis that is not dense, as the hidden states states[1:, 0] of a flashrnn_fwd call.  Returns (y, mean, rstd), the last two f32 of x.shape[:-1], or None, None."""
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
+    _chk(y, x.shape, y.dtype, "y")
+    if save_for_backward:
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
+        _chk(mean, x.shape[:-1], torch.float32, "mean")
+        _chk(rstd, x.shape[:-1], torch.float32, "rstd")
+    else:
+        mean = rstd = None
+    _same_device(x, weight=weight, bias=bias, y=y, mean=mean, rstd=rstd)
+    d = _norm_desc(x, weight, bias, y, y, eps)
+    rc = lib().flashrnn_layer_norm_fwd(ctypes.byref(d), _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream))
+    if rc != FLASHRNN_OK:
+        raise FlashRNNError(rc, "flashrnn_layer_norm_fwd")
+    return y, mean, rstd
+
+
+def flashrnn_layer_norm_bwd(dy, x, mean, rstd, weight=None, dtype=None, param_grads=True, out=None, workspace=None, stream=None):
+    """Gradient of flashrnn_layer_norm_fwd.  Returns (dx, dweight, dbias): dx dense, in dy's type or in `dtype`; the others f32 in weight's shape ([D] without a weight), or None
+    where param_grads is false.  `out` may pass preallocated (dx, dweight, dbias)."""
+    _chk(dy, x.shape, dy.dtype, "dy")
+    _chk(mean, x.shape[:-1], torch.float32, "mean")
+    _chk(rstd, x.shape[:-1], torch.float32, "rstd")
+    shape = x.shape[-1:] if weight is None else weight.shape
+    if out is None:
+        dx = torch.empty(x.shape, dtype=dy.dtype if dtype is None else dtype, device=x.device)
+        dweight, dbias = (torch.empty(shape, dtype=torch.float32, device=x.device) if param_grads else None for _ in range(2))
+    else:
+        dx, dweight, dbias = out
+        if not param_grads:
+            dweight = dbias = None
+    _chk(dx, x.shape, dx.dtype, "dx")
+    _chk(dweight, shape, torch.float32, "dweight", optional=True)
+    _chk(dbias, shape, torch.float32, "dbias", optional=True)
+    _same_device(x, dy=dy, mean=mean, rstd=rstd, weight=weight, dx=dx, dweight=dweight, dbias=dbias, workspace=workspace)
+    d = _norm_desc(x, weight, None, dy, dx, 0.0)
+    if dweight is not None or dbias is not None:
+        workspace = _sized_workspace(workspace, lib().flashrnn_layer_norm_workspace_bytes(ctypes.byref(d)), x.device)
+    rc = lib().flashrnn_layer_norm_bwd(ctypes.byref(d), _ptr(dy), _ptr(x), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                                       _stream(stream))
+    if rc != FLASHRNN_OK:
+        raise FlashRNNError(rc, "flashrnn_layer_norm_bwd")
+    return dx, dweight, dbias
+
+
+def _matrix(t, shape, dtype, name):
+    """The distance of the rows of a matrix whose rows are dense."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{name}: got {tuple(t.shape)} {t.dtype} on {t.device}, expected a device tensor {tuple(shape)} {dtype}")
+    rows, columns = shape
+    if columns > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < columns:
+        raise ValueError(f"the rows of {name} must be dense and must not overlap")
+    return max(t.stride(0), columns) if rows > 1 else columns
+
+
+def flashrnn_cross_entropy(logits, targets, dloss=None, grad_scale=1.0, gradient=True, loss=None, lse=None, dlogits=None, stream=None):
+    """Cross entropy of every row of logits[rows, classes] against targets[rows] (int64 or int32; outside the classes: ignored, loss 0), and in the same pass the
+    gradient of sum(grad_scale * dloss * loss).  dlogits may be `logits` itself; lse, where passed, takes the rows' log of the sum of exponentials.
+    Returns (loss f32[rows], dlogits in logits' type, or None where gradient is false)."""
+    N, V = logits.shape
+    stride = _matrix(logits, (N, V), logits.dtype, "logits")
+    _chk(targets, (N,), targets.dtype, "targets")
+    _chk(dloss, (N,), torch.float32, "dloss", optional=True)
+    _chk(lse, (N,), torch.float32, "lse", optional=True)
+    if loss is None:
+        loss = torch.empty(N, dtype=torch.float32, device=logits.device)
+    _chk(loss, (N,), torch.float32, "loss")
+    if not gradient:
+        dlogits = None
+    elif dlogits is None:
+        dlogits = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+    to_stride = V if dlogits is None else _matrix(dlogits, (N, V), logits.dtype, "dlogits")
+    _same_device(logits, targets=targets, dloss=dloss, loss=loss, lse=lse, dlogits=dlogits)
+    d = flashrnn_cross_entropy_desc_t(N, stride, to_stride, V, _io_dtype(logits), _index_dtype(targets), float(grad_scale))
+    rc = lib().flashrnn_cross_entropy(ctypes.byref(d), _ptr(logits), _ptr(targets), _ptr(dloss), _ptr(loss), _ptr(lse), _ptr(dlogits), _stream(stream))
+    if rc != FLASHRNN_OK:
+        raise FlashRNNError(rc, "flashrnn_cross_entropy")
+    return loss, dlogits
+
+
+def flashrnn_grad_clip(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
+    """The norm over all values of the tensors in `grads` (bf16 or f32, any mix), and the tensors scaled down so that it is max_norm at most: in place, or into the
+    tensors of `out`.  max_norm = inf computes the norm alone (and copies into `out`).  Returns norm f32[1]."""
+    grads = list(grads)
+    n = len(grads)
+    to = grads if out is None else list(out)
+    if len(to) != n:
+        raise ValueError(f"{n} gradients, {len(to)} tensors for them")
+    if norm is None:
+        if n == 0:
+            raise ValueError("norm is required where there are no gradients")
+        norm = torch.empty(1, dtype=torch.float32, device=grads[0].device)
+    _chk(norm, (1,), torch.float32, "norm")
+    for i, (g, o) in enumerate(zip(grads, to)):
+        _chk(g, g.shape, g.dtype, f"grads[{i}]")
+        if o is not g:
+            _chk(o, g.shape, g.dtype, f"out[{i}]")
+        if g.device != norm.device or o.device != norm.device:
+            raise ValueError(f"tensor {i} is on {g.device}, norm on {norm.device}")
+    workspace = _sized_workspace(workspace, lib().flashrnn_grad_clip_workspace_bytes(n), norm.device)
+    vp = ctypes.c_void_p * n
+    ins = vp(*[g.data_ptr() for g in grads])
+    outs = None if out is None and max_norm == float("inf") else vp(*[o.data_ptr() for o in to])
+    rc = lib().flashrnn_grad_clip(n, ins, outs, (ctypes.c_longlong * n)(*[g.numel() for g in grads]), (ctypes.c_int * n)(*[_io_dtype(g) for g in grads]), float(max_norm),
+                                  _ptr(norm), _ptr(workspace), _stream(stream))
+    if rc != FLASHRNN_OK:
+        raise FlashRNNError(rc, "flashrnn_grad_clip")
+    return norm
