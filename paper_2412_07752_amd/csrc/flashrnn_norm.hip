@@ -6,22 +6,26 @@ using namespace flashrnn;
 namespace {
 
 constexpr int kThreads = 256;
+// Workgroups of a forward call: 65536 x 8 x 256 states take 161 us with 768 workgroups of 256 threads, 162 with 2048, 148 with 8192 and 160 with one row for every
+// group of threads.
+constexpr unsigned kMostThreads = 8192 * 256;
 constexpr int kMaxStrips = 256;   // workgroups that add up the gradients of weight and bias, each over a strip of rows
 
 struct Rows {
-    long long inner, x_stride;
+    long long x_stride;
+    uint32_t count, per_outer;   // rows, and those of one outer block
     int groups, width;
 };
-__device__ __forceinline__ size_t x_offset(const Rows& r, size_t row) {
-    const size_t per_outer = (size_t)r.inner * r.groups;
-    return row / per_outer * r.x_stride + row % per_outer * r.width;
+__device__ __forceinline__ size_t x_offset(const Rows& r, uint32_t row) {
+    const uint32_t o = row / r.per_outer;
+    return (size_t)o * r.x_stride + (size_t)(row - o * r.per_outer) * r.width;
 }
 
 template <typename X, typename Y, typename P>
-__global__ __launch_bounds__(kThreads) void layer_norm_fwd_kernel(Rows r, size_t rows, const X* __restrict__ x, const P* __restrict__ weight, const P* __restrict__ bias, Y* __restrict__ y,
+__global__ __launch_bounds__(kThreads) void layer_norm_fwd_kernel(Rows r, const X* __restrict__ x, const P* __restrict__ weight, const P* __restrict__ bias, Y* __restrict__ y,
                                                                   float* __restrict__ mean_out, float* __restrict__ rstd_out, float eps) {
     __shared__ float lds[kThreads / kWave];
-    for (size_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    for (uint32_t row = blockIdx.x; row < r.count; row += gridDim.x) {
         const X* xr = x + x_offset(r, row);
         const int g = (int)(row % r.groups);
         float s = 0.f;
@@ -37,7 +41,7 @@ __global__ __launch_bounds__(kThreads) void layer_norm_fwd_kernel(Rows r, size_t
             float v = (load_value(xr + j) - mean) * rstd;
             if (weight) v *= load_value(weight + (size_t)g * r.width + j);
             if (bias) v += load_value(bias + (size_t)g * r.width + j);
-            store_value(y + row * r.width + j, v);
+            store_value(y + (size_t)row * r.width + j, v);
         }
         if (mean_out && threadIdx.x == 0) {
             mean_out[row] = mean;
@@ -46,14 +50,131 @@ __global__ __launch_bounds__(kThreads) void layer_norm_fwd_kernel(Rows r, size_t
     }
 }
 
+// Rows in registers.  A row is read once: a group of L threads (lanes of a wave, or a whole workgroup) holds it as K chunks of V values a thread, chunk
+// k of thread l being number k * L + l.  The last chunk of a row whose length is no multiple of V ends with the row and overlaps the one before it: the values that both
+// hold count once in the sums and are stored twice, the same.  Threads beyond the last chunk hold that chunk too, count nothing and store nothing.  Groups
+// take rows a fixed number apart, which is a multiple of `groups`, so that a thread's part of weight and bias stays in its registers; the next row's loads are on
+// their way while this row is worked on.
+template <int L> constexpr int threads_of() { return L <= kWave ? kThreads : L; }
+
+template <int L, int K, int V> struct RowPart {
+    int at[K];      // first value of each chunk
+    int skip;       // values at the start of chunk K - 1 that the chunk before it holds (V: all, nothing is stored)
+    __device__ __forceinline__ RowPart(int l, int width) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) at[k] = (k * L + l) * V;
+        const int last = width - V;
+        skip = at[K - 1] > last ? (at[K - 1] < width ? at[K - 1] - last : V) : 0;
+        at[K - 1] = at[K - 1] > last ? last : at[K - 1];
+    }
+    __device__ __forceinline__ bool counts(int k, int i) const { return k < K - 1 || i >= skip; }
+    __device__ __forceinline__ bool stores(int k) const { return k < K - 1 || skip < V; }
+};
+
+template <typename X, int V, int L, int K>
+__global__ __launch_bounds__(threads_of<L>()) void layer_norm_rows_kernel(Rows r, const X* __restrict__ x, const void* __restrict__ weight, const void* __restrict__ bias,
+                                                                         bool params_bf16, void* __restrict__ y, bool y_bf16, bool stream, float* __restrict__ mean_out,
+                                                                         float* __restrict__ rstd_out, float eps) {
+    constexpr int NT = threads_of<L>(), PER = NT / L;   // groups of threads in a workgroup
+    __shared__ float slots[2][NT / kWave];
+    const int l = threadIdx.x % L;
+    const uint32_t stride = gridDim.x * PER, first = blockIdx.x * PER + threadIdx.x / L;
+    const uint32_t lead = L <= kWave ? blockIdx.x * PER + threadIdx.x / kWave * (kWave / L) : first;   // the wave's first row
+    const RowPart<L, K, V> part(l, r.width);
+    float w[K][V], b[K][V];
+    const size_t own = (size_t)(first % r.groups) * r.width;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (weight) load_chunk<V>(weight, params_bf16, own + part.at[k], w[k]);
+        else
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[k][i] = 1.f;
+        if (bias) load_chunk<V>(bias, params_bf16, own + part.at[k], b[k]);
+        else
+#pragma unroll
+            for (int i = 0; i < V; ++i) b[k][i] = 0.f;
+    }
+    Chunk<X, V> raw[K];
+    auto fetch = [&](uint32_t row) __attribute__((always_inline)) {
+        const X* p = x + x_offset(r, row < r.count ? row : r.count - 1);
+#pragma unroll
+        for (int k = 0; k < K; ++k) raw[k].load(p + part.at[k]);
+    };
+    fetch(first);
+    const float n = (float)r.width;
+    for (uint32_t base = lead, row = first; base < r.count; base += stride, row += stride) {
+        float v[K][V], s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                v[k][i] = raw[k].get(i);
+                s += part.counts(k, i) ? v[k][i] : 0.f;
+            }
+        if (base + stride < r.count) fetch(row + stride);
+        const float mean = group_sum<L>(s, slots[0]) / n;
+        s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                v[k][i] -= mean;
+                s += part.counts(k, i) ? v[k][i] * v[k][i] : 0.f;
+            }
+        const float rstd = 1.0f / sqrtf(group_sum<L>(s, slots[1]) / n + eps);
+        if (row < r.count) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[k][i] = v[k][i] * rstd * w[k][i] + b[k][i];
+                if (part.stores(k)) store_chunk<V>(y, y_bf16, (size_t)row * r.width + part.at[k], v[k], stream);
+            }
+            if (mean_out && l == 0) {
+                mean_out[row] = mean;
+                rstd_out[row] = rstd;
+            }
+        }
+    }
+}
+
+// calls f(L, K) as compile-time constants: the smallest group that holds `chunks` chunks, in waves' lanes first, then workgroups; false if none does
+template <int A, int B> struct Shape { static constexpr int L = A, K = B; };
+template <typename F> bool with_shape(int chunks, F&& f) {
+    bool done = false;
+    auto take = [&](auto s) {
+        if (!done && chunks <= decltype(s)::L * decltype(s)::K) {
+            f(s);
+            done = true;
+        }
+    };
+    take(Shape<8, 1>{}); take(Shape<8, 2>{}); take(Shape<8, 3>{}); take(Shape<8, 4>{}); take(Shape<16, 3>{}); take(Shape<16, 4>{}); take(Shape<32, 3>{}); take(Shape<32, 4>{});
+    take(Shape<64, 3>{}); take(Shape<64, 4>{}); take(Shape<256, 2>{}); take(Shape<256, 3>{}); take(Shape<256, 4>{}); take(Shape<512, 3>{}); take(Shape<512, 4>{});
+    return done;
+}
+// workgroups of PER groups of threads each: at most `most`, and a number that keeps a group's rows on one row of the weights
+inline unsigned blocks_for(size_t rows, int per, int groups, unsigned most) {
+    const size_t want = (rows + per - 1) / per;
+    if (want <= most) return (unsigned)want;
+    int a = groups, b = per;
+    while (b) {
+        const int t = a % b;
+        a = b;
+        b = t;
+    }
+    const size_t unit = groups / a;
+    if (unit > (1u << 20)) return 0;   // (a dispatch holds fewer than 2^32 threads)
+    const size_t blocks = most < unit ? unit : most / unit * unit;
+    return (unsigned)(blocks < want ? blocks : want);
+}
+
 template <typename X, typename Y, typename DX, typename P>
-__global__ __launch_bounds__(kThreads) void layer_norm_dx_kernel(Rows r, size_t rows, const Y* __restrict__ dy, const X* __restrict__ x, const P* __restrict__ weight,
+__global__ __launch_bounds__(kThreads) void layer_norm_dx_kernel(Rows r, const Y* __restrict__ dy, const X* __restrict__ x, const P* __restrict__ weight,
                                                                  const float* __restrict__ mean_in, const float* __restrict__ rstd_in, DX* __restrict__ dx) {
     __shared__ float lds[kThreads / kWave];
-    for (size_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    for (uint32_t row = blockIdx.x; row < r.count; row += gridDim.x) {
         const X* xr = x + x_offset(r, row);
-        const Y* dyr = dy + row * r.width;
-        const P* w = weight ? weight + row % r.groups * r.width : nullptr;
+        const Y* dyr = dy + (size_t)row * r.width;
+        const P* w = weight ? weight + (size_t)(row % r.groups) * r.width : nullptr;
         const float mean = mean_in[row], rstd = rstd_in[row];
         float a = 0.f, b = 0.f;
         for (int j = threadIdx.x; j < r.width; j += kThreads) {
@@ -65,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void layer_norm_dx_kernel(Rows r, size_t 
         b = block_sum<kThreads>(b, lds) / r.width;
         for (int j = threadIdx.x; j < r.width; j += kThreads) {
             const float g = load_value(dyr + j) * (w ? load_value(w + j) : 1.0f);
-            store_value(dx + row * r.width + j, rstd * (g - a - (load_value(xr + j) - mean) * rstd * b));
+            store_value(dx + (size_t)row * r.width + j, rstd * (g - a - (load_value(xr + j) - mean) * rstd * b));
         }
     }
 }
@@ -79,8 +200,8 @@ __global__ __launch_bounds__(kThreads) void layer_norm_dparam_kernel(Rows r, siz
     const int g = (int)(col / r.width), j = (int)(col % r.width);
     float dw = 0.f, db = 0.f;
     for (size_t t = blockIdx.y; t < tokens; t += gridDim.y) {
-        const size_t row = t * r.groups + g;
-        const float d = load_value(dy + row * r.width + j);
+        const uint32_t row = (uint32_t)t * r.groups + g;
+        const float d = load_value(dy + (size_t)row * r.width + j);
         dw += d * ((load_value(x + x_offset(r, row) + j) - mean_in[row]) * rstd_in[row]);
         db += d;
     }
@@ -107,7 +228,10 @@ int check_desc(const flashrnn_layer_norm_desc_t* d) {
     if (rows > 2147483647.0 || extent > 1e18 || (double)d->groups * d->width > 2147483647.0) return FLASHRNN_ERR_UNSUPPORTED;
     return FLASHRNN_OK;
 }
-size_t rows_of(const flashrnn_layer_norm_desc_t* d) { return (size_t)d->rows_outer * d->rows_inner * d->groups; }
+Rows rows_of(const flashrnn_layer_norm_desc_t* d) {
+    const size_t per_outer = (size_t)d->rows_inner * d->groups;   // (both below 2^31, or there are no rows)
+    return Rows{d->x_stride, (uint32_t)(d->rows_outer * per_outer), (uint32_t)per_outer, d->groups, d->width};
+}
 int strips_of(const flashrnn_layer_norm_desc_t* d) {
     const size_t tokens = (size_t)d->rows_outer * d->rows_inner;
     return tokens < kMaxStrips ? (tokens ? (int)tokens : 1) : kMaxStrips;
@@ -126,20 +250,36 @@ size_t flashrnn_layer_norm_workspace_bytes(const flashrnn_layer_norm_desc_t* d) 
 int flashrnn_layer_norm_fwd(const flashrnn_layer_norm_desc_t* d, const void* x, const void* weight, const void* bias, void* y, void* mean, void* rstd, void* hip_stream) {
     const int rc = check_desc(d);
     if (rc != FLASHRNN_OK) return rc;
-    const size_t rows = rows_of(d);
+    const Rows r = rows_of(d);
+    const size_t rows = r.count;
     if (rows == 0) return FLASHRNN_OK;
     if (!x || !y || (mean == nullptr) != (rstd == nullptr)) return FLASHRNN_ERR_NULL;
     if (!aligned_to(x, type_size(d->x_dtype)) || !aligned_to(y, type_size(d->io_dtype)) || !aligned_to(weight, type_size(d->param_dtype)) ||
         !aligned_to(bias, type_size(d->param_dtype)) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
         return FLASHRNN_ERR_UNSUPPORTED;
-    const Rows r{d->rows_inner, d->x_stride, d->groups, d->width};
+    int status = FLASHRNN_OK;
+    bool taken = false;
+    if (d->width >= 8) with_io_type(d->x_dtype, [&](auto* xt) {
+        using X = std::remove_pointer_t<decltype(xt)>;
+        constexpr int V = 16 / sizeof(X);
+        return (int)with_shape((d->width + V - 1) / V, [&](auto s) {
+            constexpr int L = decltype(s)::L, K = decltype(s)::K, NT = threads_of<L>();
+            const unsigned blocks = blocks_for(rows, NT / L, d->groups, kMostThreads / NT);
+            if (!blocks) return;
+            taken = true;
+            hipLaunchKernelGGL((layer_norm_rows_kernel<X, V, L, K>), dim3(blocks), dim3(NT), 0, (hipStream_t)hip_stream, r, (const X*)x, weight, bias,
+                               d->param_dtype == FLASHRNN_BF16, y, d->io_dtype == FLASHRNN_BF16, rows * d->width * type_size(d->io_dtype) > kStreamBytes, (float*)mean, (float*)rstd, d->eps);
+            status = launch_status();
+        });
+    });
+    if (taken) return status;
     return with_io_type(d->x_dtype, [&](auto* xt) {
         return with_io_type(d->io_dtype, [&](auto* yt) {
             return with_io_type(d->param_dtype, [&](auto* pt) {
                 using X = std::remove_pointer_t<decltype(xt)>;
                 using Y = std::remove_pointer_t<decltype(yt)>;
                 using P = std::remove_pointer_t<decltype(pt)>;
-                hipLaunchKernelGGL((layer_norm_fwd_kernel<X, Y, P>), dim3(row_blocks(rows)), dim3(kThreads), 0, (hipStream_t)hip_stream, r, rows, (const X*)x, (const P*)weight,
+                hipLaunchKernelGGL((layer_norm_fwd_kernel<X, Y, P>), dim3(row_blocks(rows)), dim3(kThreads), 0, (hipStream_t)hip_stream, r, (const X*)x, (const P*)weight,
                                    (const P*)bias, (Y*)y, (float*)mean, (float*)rstd, d->eps);
                 return launch_status();
             });
@@ -151,14 +291,14 @@ int flashrnn_layer_norm_bwd(const flashrnn_layer_norm_desc_t* d, const void* dy,
                             void* dbias, void* workspace, void* hip_stream) {
     int rc = check_desc(d);
     if (rc != FLASHRNN_OK) return rc;
-    const size_t rows = rows_of(d), columns = (size_t)d->groups * d->width, tokens = rows / d->groups;
+    const Rows r = rows_of(d);
+    const size_t rows = r.count, columns = (size_t)d->groups * d->width, tokens = rows / d->groups;
     if (rows && (!dy || !x || !mean || !rstd || !dx)) return FLASHRNN_ERR_NULL;
     const bool params = dweight || dbias;
     if (params && (!workspace || !aligned_to(workspace, 256))) return FLASHRNN_ERR_WORKSPACE;
     if (!aligned_to(x, type_size(d->x_dtype)) || !aligned_to(dy, type_size(d->io_dtype)) || !aligned_to(dx, type_size(d->dx_dtype)) ||
         !aligned_to(weight, type_size(d->param_dtype)) || !aligned_to(mean, 4) || !aligned_to(rstd, 4) || !aligned_to(dweight, 4) || !aligned_to(dbias, 4))
         return FLASHRNN_ERR_UNSUPPORTED;
-    const Rows r{d->rows_inner, d->x_stride, d->groups, d->width};
     const hipStream_t stream = (hipStream_t)hip_stream;
     const unsigned column_blocks = (unsigned)((columns + kThreads - 1) / kThreads);
     rc = with_io_type(d->x_dtype, [&](auto* xt) {
@@ -175,7 +315,7 @@ int flashrnn_layer_norm_bwd(const flashrnn_layer_norm_desc_t* d, const void* dy,
                 return with_io_type(d->param_dtype, [&](auto* pt) {
                     using DX = std::remove_pointer_t<decltype(dt)>;
                     using P = std::remove_pointer_t<decltype(pt)>;
-                    hipLaunchKernelGGL((layer_norm_dx_kernel<X, Y, DX, P>), dim3(row_blocks(rows)), dim3(kThreads), 0, stream, r, rows, (const Y*)dy, (const X*)x, (const P*)weight,
+                    hipLaunchKernelGGL((layer_norm_dx_kernel<X, Y, DX, P>), dim3(row_blocks(rows)), dim3(kThreads), 0, stream, r, (const Y*)dy, (const X*)x, (const P*)weight,
                                        (const float*)mean, (const float*)rstd, (DX*)dx);
                     return launch_status();
                 });
