@@ -9,6 +9,9 @@ constexpr int kThreads = 256;
 // Workgroups of a forward call: 65536 x 8 x 256 states take 161 us with 768 workgroups of 256 threads, 162 with 2048, 148 with 8192 and 160 with one row for every
 // group of threads.
 constexpr unsigned kMostThreads = 8192 * 256;
+// ... and of a gradient, whose workgroups each leave partial sums of dweight and dbias: 16384 x 768 values in bf16 take 19.8 us with 512 workgroups of 256 threads, 23 with 768,
+// 25 with 1024 and 32 with 2048; 65536 x 8 x 256 states 210, 218, 234 and 236.
+constexpr unsigned kMostGradThreads = 512 * 256;
 constexpr int kMaxStrips = 256;   // workgroups that add up the gradients of weight and bias, each over a strip of rows
 
 struct Rows {
@@ -137,6 +140,158 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_rows_kernel(Rows r
     }
 }
 
+// The gradient, rows in registers as above: dx from the row's two sums, and every thread's part of dweight and dbias in its registers over all rows that its group takes.
+// At the end the groups of a workgroup that share a row of the weights meet in LDS and their sum, in the order of the groups, is one row of partial sums; with more
+// rows of weights than groups every group writes its own.  sums: [dweight, dbias][strips][groups][width], a strip for every workgroup, or for every `groups` groups of threads.
+template <typename X, typename Y, int V, int L, int K>
+__global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(Rows r, const Y* __restrict__ dy, const X* __restrict__ x, const void* __restrict__ weight,
+                                                                              bool weight_bf16, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
+                                                                              void* __restrict__ dx, bool dx_bf16, bool stream, float* __restrict__ sums, size_t sum_rows) {
+    constexpr int NT = threads_of<L>(), PER = NT / L;
+    __shared__ float slots[2][2][NT / kWave];
+    __shared__ float merge[PER > 1 ? NT * K * V : 1];
+    const int l = threadIdx.x % L, group = threadIdx.x / L;
+    const uint32_t stride = gridDim.x * PER, first = blockIdx.x * PER + group;
+    const uint32_t lead = L <= kWave ? blockIdx.x * PER + threadIdx.x / kWave * (kWave / L) : first;
+    const RowPart<L, K, V> part(l, r.width);
+    float w[K][V], dw[K][V], db[K][V];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (weight) load_chunk<V>(weight, weight_bf16, (size_t)(first % r.groups) * r.width + part.at[k], w[k]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if (!weight) w[k][i] = 1.f;
+            dw[k][i] = db[k][i] = 0.f;
+        }
+    }
+    Chunk<X, V> raw_x[K];
+    Chunk<Y, V> raw_dy[K];
+    float mean = 0.f, rstd = 0.f;
+    auto fetch = [&](uint32_t row) __attribute__((always_inline)) {
+        row = row < r.count ? row : r.count - 1;
+        const X* p = x + x_offset(r, row);
+        const Y* q = dy + (size_t)row * r.width;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            raw_x[k].load(p + part.at[k]);
+            raw_dy[k].load(q + part.at[k]);
+        }
+        mean = mean_in[row];
+        rstd = rstd_in[row];
+    };
+    fetch(first);
+    const float n = (float)r.width;
+    int turn = 0;
+    for (uint32_t base = lead, row = first; base < r.count; base += stride, row += stride, turn ^= 1) {
+        float xh[K][V], g[K][V], a = 0.f, b = 0.f;
+        const float scale = rstd;
+        const bool there = row < r.count;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                xh[k][i] = (raw_x[k].get(i) - mean) * rstd;
+                g[k][i] = raw_dy[k].get(i);
+                if (there) {   // (of a chunk's values that another one holds too, the other one's sums are written)
+                    dw[k][i] += g[k][i] * xh[k][i];
+                    db[k][i] += g[k][i];
+                }
+                g[k][i] *= w[k][i];
+                a += part.counts(k, i) ? g[k][i] : 0.f;
+                b += part.counts(k, i) ? g[k][i] * xh[k][i] : 0.f;
+            }
+        if (base + stride < r.count) fetch(row + stride);
+        if constexpr (L <= kWave) {
+            a = lanes_sum<L>(a);
+            b = lanes_sum<L>(b);
+        } else {   // (both sums behind one barrier; the slots alternate)
+            a = lanes_sum<kWave>(a);
+            b = lanes_sum<kWave>(b);
+            if ((threadIdx.x & 63) == 0) {
+                slots[turn][0][threadIdx.x >> 6] = a;
+                slots[turn][1][threadIdx.x >> 6] = b;
+            }
+            __syncthreads();
+            a = slots[turn][0][0];
+            b = slots[turn][1][0];
+#pragma unroll
+            for (int i = 1; i < NT / kWave; ++i) {
+                a += slots[turn][0][i];
+                b += slots[turn][1][i];
+            }
+        }
+        a /= n;
+        b /= n;
+        if (there) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) g[k][i] = scale * (g[k][i] - a - xh[k][i] * b);
+                if (part.stores(k)) store_chunk<V>(dx, dx_bf16, (size_t)row * r.width + part.at[k], g[k], stream);
+            }
+        }
+    }
+    if (!sums) return;
+    const bool shared = r.groups <= PER;
+    const uint32_t to = shared ? blockIdx.x * r.groups + first % r.groups : first;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float(&v)[K][V] = which ? db : dw;
+        if (PER > 1 && shared) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) merge[(k * V + i) * NT + threadIdx.x] = v[k][i];
+            __syncthreads();
+            if (group < r.groups)
+                for (int other = group + r.groups; other < PER; other += r.groups)
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) v[k][i] += merge[(k * V + i) * NT + other * L + l];
+        }
+        if (!shared || group < r.groups) {
+            float* out = sums + (which * sum_rows + to) * r.width;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (part.stores(k)) {
+                    Chunk<float, V> c;
+                    c.put(v[k]);
+                    c.store(out + part.at[k]);
+                }
+        }
+    }
+}
+
+// dweight and dbias from partial sums [dweight, dbias][strips][columns]: a wave adds up every kSumWaves-th strip of 64 columns, in order, then the waves meet
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(kSumWaves * kWave) void layer_norm_sum_strips_kernel(const float* __restrict__ part, size_t columns, int strips, float* __restrict__ dweight,
+                                                                                 float* __restrict__ dbias) {
+    __shared__ float lds[kSumWaves][kWave];
+    float* out = blockIdx.y ? dbias : dweight;
+    if (!out) return;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const size_t col = (size_t)blockIdx.x * kWave + lane;
+    const float* p = part + (size_t)blockIdx.y * strips * columns + (col < columns ? col : columns - 1);
+    float s = 0.f;
+    int i = w;
+    for (; i + 7 * kSumWaves < strips; i += 8 * kSumWaves) {   // eight loads on their way
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = p[(size_t)(i + u * kSumWaves) * columns];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; i < strips; i += kSumWaves) s += p[(size_t)i * columns];
+    lds[w][lane] = s;
+    __syncthreads();
+    if (w == 0 && col < columns) {
+        for (int u = 1; u < kSumWaves; ++u) s += lds[u][lane];
+        out[col] = s;
+    }
+}
+
 // calls f(L, K) as compile-time constants: the smallest group that holds `chunks` chunks, in waves' lanes first, then workgroups; false if none does
 template <int A, int B> struct Shape { static constexpr int L = A, K = B; };
 template <typename F> bool with_shape(int chunks, F&& f) {
@@ -152,19 +307,37 @@ template <typename F> bool with_shape(int chunks, F&& f) {
     return done;
 }
 // workgroups of PER groups of threads each: at most `most`, and a number that keeps a group's rows on one row of the weights
-inline unsigned blocks_for(size_t rows, int per, int groups, unsigned most) {
-    const size_t want = (rows + per - 1) / per;
-    if (want <= most) return (unsigned)want;
-    int a = groups, b = per;
-    while (b) {
-        const int t = a % b;
-        a = b;
-        b = t;
+inline size_t lcm_of(size_t a, size_t b) {
+    size_t x = a, y = b;
+    while (y) {
+        const size_t t = x % y;
+        x = y;
+        y = t;
     }
-    const size_t unit = groups / a;
+    return a / x * b;
+}
+inline unsigned blocks_for(size_t rows, int per, int groups, unsigned most) {
+    const size_t want = (rows + per - 1) / per, unit = lcm_of(groups, per) / per;
+    if (want <= most) return (unsigned)want;
     if (unit > (1u << 20)) return 0;   // (a dispatch holds fewer than 2^32 threads)
     const size_t blocks = most < unit ? unit : most / unit * unit;
     return (unsigned)(blocks < want ? blocks : want);
+}
+
+// launch of the gradient with rows in registers; blocks = 0: none
+struct GradPlan {
+    unsigned blocks;
+    size_t sum_rows;   // rows of partial sums
+};
+inline GradPlan grad_plan(const Rows& r, int per, int threads) {
+    GradPlan p{blocks_for(r.count, per, r.groups, kMostGradThreads / threads), 0};
+    if (r.groups > per) {   // whole strips: workgroups beyond the rows write zeros
+        const size_t unit = lcm_of(r.groups, per) / per;
+        p.blocks = unit > (1u << 20) ? 0 : (unsigned)((p.blocks + unit - 1) / unit * unit);
+    }
+    if ((size_t)r.groups * r.width > (1u << 27)) p.blocks = 0;   // (a dispatch holds fewer than 2^32 threads, the sum's too)
+    p.sum_rows = (size_t)p.blocks * (r.groups <= per ? r.groups : per);
+    return p;
 }
 
 template <typename X, typename Y, typename DX, typename P>
@@ -225,7 +398,7 @@ int check_desc(const flashrnn_layer_norm_desc_t* d) {
     if (!is_io_type(d->x_dtype) || !is_io_type(d->io_dtype) || !is_io_type(d->dx_dtype) || !is_io_type(d->param_dtype)) return FLASHRNN_ERR_SHAPE;
     // rows below 2^31 (one workgroup each at most), every offset in bytes below 2^62
     const double rows = (double)d->rows_outer * (double)d->rows_inner * d->groups, extent = (double)d->rows_outer * (double)d->x_stride + rows * d->width;
-    if (rows > 2147483647.0 || extent > 1e18 || (double)d->groups * d->width > 2147483647.0) return FLASHRNN_ERR_UNSUPPORTED;
+    if (rows > 2147483647.0 || extent > 1e18 || (double)d->groups * d->width > 1073741824.0) return FLASHRNN_ERR_UNSUPPORTED;
     return FLASHRNN_OK;
 }
 Rows rows_of(const flashrnn_layer_norm_desc_t* d) {
@@ -237,14 +410,31 @@ int strips_of(const flashrnn_layer_norm_desc_t* d) {
     return tokens < kMaxStrips ? (tokens ? (int)tokens : 1) : kMaxStrips;
 }
 
+template <int N> struct Int { static constexpr int value = N; };
+// calls f(X*, Y*, V, shape) for a gradient whose rows fit in registers
+template <typename F> void with_grad_shape(const flashrnn_layer_norm_desc_t* d, F&& f) {
+    if (d->width < 8) return;
+    with_io_type(d->x_dtype, [&](auto* xt) {
+        return with_io_type(d->io_dtype, [&](auto* yt) {
+            constexpr int V = sizeof(*xt) == 2 && sizeof(*yt) == 2 ? 8 : 4;
+            return (int)with_shape((d->width + V - 1) / V, [&](auto s) { f(xt, yt, Int<V>{}, s); });
+        });
+    });
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t flashrnn_layer_norm_workspace_bytes(const flashrnn_layer_norm_desc_t* d) {
     if (check_desc(d) != FLASHRNN_OK) return 0;
-    const size_t bytes = (size_t)strips_of(d) * 2 * d->groups * d->width * sizeof(float);
-    return (bytes + 255) / 256 * 256;
+    size_t rows = (size_t)strips_of(d) * d->groups;
+    with_grad_shape(d, [&](auto, auto, auto, auto s) {
+        constexpr int NT = threads_of<decltype(s)::L>();
+        const GradPlan p = grad_plan(rows_of(d), NT / decltype(s)::L, NT);
+        if (p.sum_rows) rows = p.sum_rows;
+    });
+    return (rows * 2 * d->width * sizeof(float) + 255) / 256 * 256;
 }
 
 int flashrnn_layer_norm_fwd(const flashrnn_layer_norm_desc_t* d, const void* x, const void* weight, const void* bias, void* y, void* mean, void* rstd, void* hip_stream) {
@@ -300,6 +490,27 @@ int flashrnn_layer_norm_bwd(const flashrnn_layer_norm_desc_t* d, const void* dy,
         !aligned_to(weight, type_size(d->param_dtype)) || !aligned_to(mean, 4) || !aligned_to(rstd, 4) || !aligned_to(dweight, 4) || !aligned_to(dbias, 4))
         return FLASHRNN_ERR_UNSUPPORTED;
     const hipStream_t stream = (hipStream_t)hip_stream;
+    bool taken = false;
+    int strips = 0;
+    if (rows) with_grad_shape(d, [&](auto* xt, auto* yt, auto v, auto s) {
+        using X = std::remove_pointer_t<decltype(xt)>;
+        using Y = std::remove_pointer_t<decltype(yt)>;
+        constexpr int L = decltype(s)::L, K = decltype(s)::K, NT = threads_of<L>();
+        const GradPlan p = grad_plan(r, NT / L, NT);
+        if (!p.blocks) return;
+        taken = true;
+        strips = (int)(p.sum_rows / r.groups);
+        hipLaunchKernelGGL((layer_norm_grad_rows_kernel<X, Y, decltype(v)::value, L, K>), dim3(p.blocks), dim3(NT), 0, stream, r, (const Y*)dy, (const X*)x, weight,
+                           d->param_dtype == FLASHRNN_BF16, (const float*)mean, (const float*)rstd, dx, d->dx_dtype == FLASHRNN_BF16,
+                           rows * d->width * type_size(d->dx_dtype) > kStreamBytes, params ? (float*)workspace : nullptr, p.sum_rows);
+        rc = launch_status();
+    });
+    if (taken) {
+        if (rc != FLASHRNN_OK || !params) return rc;
+        hipLaunchKernelGGL(layer_norm_sum_strips_kernel, dim3((unsigned)((columns + kWave - 1) / kWave), 2), dim3(kSumWaves * kWave), 0, stream, (const float*)workspace, columns,
+                           strips, (float*)dweight, (float*)dbias);
+        return launch_status();
+    }
     const unsigned column_blocks = (unsigned)((columns + kThreads - 1) / kThreads);
     rc = with_io_type(d->x_dtype, [&](auto* xt) {
         return with_io_type(d->io_dtype, [&](auto* yt) {
