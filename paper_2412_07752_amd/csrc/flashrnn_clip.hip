@@ -5,7 +5,6 @@ using namespace flashrnn;
 
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kTensors = 128;      // tensors per launch: their table is a kernel argument, which holds 4 KB
 constexpr int kMaxBlocks = 2048;   // workgroups per launch, each with a partial sum
 constexpr int kChunk = 8192;       // values of one tensor that a workgroup takes at a time

@@ -10,7 +10,6 @@ using namespace flashrnn;
 
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kDigitBits = 8;
 constexpr int kDigits = 1 << kDigitBits;

@@ -1,41 +1,168 @@
 // Cross entropy of rows of logits and its gradient (include/flashrnn.h).
+//
+// loss = lse - x_t and dx_j = f (exp(x_j - top) / s - [j = t]) with top the row's largest logit, s = sum exp(x_j - top), lse = top + log s, f = grad_scale * dloss.  The call is
+// bound by memory: a row is read once and its gradient written once, and in between it stays in registers as it lies in memory (16 bytes of it per word of four registers); the exponentials are
+// formed twice rather than kept.
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr float kLog2e = 1.44269504088896340736f;
 
-template <typename X, typename I>
-__global__ __launch_bounds__(kThreads) void cross_entropy_kernel(size_t rows, int classes, size_t x_stride, size_t dx_stride, const X* logits, const I* __restrict__ targets,
-                                                                 const float* __restrict__ dloss, float scale, float* __restrict__ loss, float* __restrict__ lse_out, X* dlogits) {
-    __shared__ float lds[kThreads / kWave];
-    for (size_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        const X* x = logits + row * x_stride;
-        const int64_t target = targets[row];
-        const bool counts = target >= 0 && target < classes;
-        // the largest logit; fmaxf passes over NaN, which the sum then holds
-        float top = -__builtin_inff();
-        for (int j = threadIdx.x; j < classes; j += kThreads) top = fmaxf(top, load_value(x + j));
-        top = block_max<kThreads>(top, lds);
+struct Problem {
+    const void *logits, *targets;
+    const float* dloss;
+    float *loss, *lse;
+    void* dlogits;
+    size_t rows, stride, to_stride;
+    int classes, index64, stream;
+    float scale;
+};
+__device__ __forceinline__ int64_t target_of(const Problem& p, size_t row) { return p.index64 ? ((const int64_t*)p.targets)[row] : ((const int32_t*)p.targets)[row]; }
+// exp(x - top): the difference first, so that no finite logit overflows on the way
+__device__ __forceinline__ float exp_below(float x, float top) { return fast_exp2((x - top) * kLog2e); }
+
+// Groups of L threads hold a row as K chunks of V values each, laid out as RowPart says.  Up to 7 chunks (57344 classes in bf16) the kernel keeps to 64 registers, so that a CU holds two
+// workgroups of 1024 threads and one's loads and stores run beside the other's arithmetic: 16384 x 50304 in bf16 565 us (5.8 TB/s), with one workgroup 653; eight chunks do not fit.
+template <typename X, int L, int K>
+__global__ __launch_bounds__(threads_of<L>(), L == 1024 && K <= 7 ? 8 : 1) void loss_rows_kernel(Problem p) {
+    constexpr int V = 16 / sizeof(X), NT = threads_of<L>(), PER = NT / L;
+    __shared__ float slots[2][NT / kWave];
+    const int l = threadIdx.x % L;
+    const RowPart<L, K, V> part(l, p.classes);
+    for (size_t base = (size_t)blockIdx.x * PER + (L <= kWave ? threadIdx.x / kWave * (kWave / L) : 0); base < p.rows; base += (size_t)gridDim.x * PER) {
+        const size_t row = L <= kWave ? base + threadIdx.x % kWave / L : base;
+        const bool there = row < p.rows;
+        const int64_t t = there ? target_of(p, row) : -1;
+        const bool counts = t >= 0 && t < p.classes;
+        const int target = counts ? (int)t : -1;
+        Chunk<X, V> raw[K];
+        if (counts || (there && p.lse)) {   // (an ignored row is not read)
+            const X* x = (const X*)p.logits + row * p.stride;
+#pragma unroll
+            for (int k = 0; k < K; ++k) raw[k].load(x + part.at[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) raw[k].clear();
+        }
+        float top = raw[0].get(0);   // fmaxf passes over NaN, which the sum then holds
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = fmaxf(top, raw[k].get(i));
+        top = group_max<L>(top, slots[0]);
         if (top == -__builtin_inff()) top = 0.f;   // (nothing but -inf, whose terms are all 0 then, or NaN)
         float s = 0.f;
-        for (int j = threadIdx.x; j < classes; j += kThreads) s += expf(load_value(x + j) - top);
-        s = block_sum<kThreads>(s, lds);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            raw[k].refresh();
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float e = exp_below(raw[k].get(i), top);
+                s += part.counts(k, i) ? e : 0.f;
+            }
+        }
+        s = group_sum<L>(s, slots[1]);
+        if (!there) continue;
         const float lse = logf(s) + top;
+        if (l == 0) {
+            if (p.lse) p.lse[row] = lse;
+            if (!counts) p.loss[row] = 0.f;
+        }
+        const float f = p.scale * (p.dloss ? p.dloss[row] : 1.f), fs = f / s;
+        const bool zero = !counts || s == 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            raw[k].refresh();
+            const int hit = target - part.at[k];   // the target's place in this chunk, where it holds it
+            const bool holds = counts && hit >= 0 && hit < V;
+            float g[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[i] = zero ? 0.f : fs * exp_below(raw[k].get(i), top);
+            if (holds) {
+                float x = 0.f;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (i == hit) {
+                        x = raw[k].get(i);
+                        if (!zero) g[i] -= f;
+                    }
+                if (part.stores(k)) p.loss[row] = s == 0.f ? __builtin_inff() : lse - x;
+            }
+            if (p.dlogits && part.stores(k)) {
+                Chunk<X, V> c;
+                c.put(g);
+                c.store((X*)p.dlogits + row * p.to_stride + part.at[k], p.stream);
+            }
+        }
+    }
+}
+
+// Rows that no group's registers hold, and rows shorter than a chunk: read twice, the sum kept up with a running maximum.
+template <typename X, int NT>
+__global__ __launch_bounds__(NT) void loss_long_kernel(Problem p) {
+    constexpr int V = 16 / sizeof(X);
+    __shared__ float slots[2][NT / kWave];
+    const int whole = p.classes / V * V, tail = whole + threadIdx.x;   // (chunks, then a value each)
+    for (size_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const X* x = (const X*)p.logits + row * p.stride;
+        X* dx = (X*)p.dlogits + row * p.to_stride;
+        const int64_t t = target_of(p, row);
+        const bool counts = t >= 0 && t < p.classes;
+        float top = -__builtin_inff(), s = 0.f;
+        auto add = [&](float v, float m) { s += exp_below(v, m); };
+        auto raise = [&](float m) {   // a larger maximum: what is there shrinks
+            if (m > top) {
+                s = s == 0.f ? 0.f : s * exp_below(top, m);
+                top = m;
+            }
+        };
+        for (int at = threadIdx.x * V; at < whole; at += NT * V) {
+            Chunk<X, V> c;
+            c.load(x + at);
+            float m = c.get(0);
+#pragma unroll
+            for (int i = 1; i < V; ++i) m = fmaxf(m, c.get(i));
+            raise(m);
+#pragma unroll
+            for (int i = 0; i < V; ++i) add(c.get(i), top == -__builtin_inff() ? 0.f : top);
+        }
+        if (tail < p.classes) {
+            const float v = load_value(x + tail);
+            raise(v);
+            add(v, top == -__builtin_inff() ? 0.f : top);
+        }
+        float all = group_max<NT>(top, slots[0]);
+        if (all == -__builtin_inff()) all = 0.f;
+        s = top == -__builtin_inff() ? s : s * exp_below(top, all);   // (a thread without a maximum holds 0, or NaN)
+        s = group_sum<NT>(s, slots[1]);
+        const float lse = logf(s) + all, f = p.scale * (p.dloss ? p.dloss[row] : 1.f), fs = f / s;
+        const bool zero = !counts || s == 0.f;
         if (threadIdx.x == 0) {
-            loss[row] = !counts ? 0.f : s == 0.f ? __builtin_inff() : lse - load_value(x + target);
-            if (lse_out) lse_out[row] = lse;
+            if (p.lse) p.lse[row] = lse;
+            if (!counts) p.loss[row] = 0.f;
         }
-        if (!dlogits) continue;
-        __syncthreads();   // (thread 0 has read the target's logit, which an output in place overwrites)
-        X* dx = dlogits + row * dx_stride;
-        const float factor = scale * (dloss ? dloss[row] : 1.f);
-        for (int j = threadIdx.x; j < classes; j += kThreads) {
-            const float p = expf(load_value(x + j) - top) / s;
-            store_value(dx + j, counts && s != 0.f ? factor * (p - (j == target ? 1.f : 0.f)) : 0.f);
+        auto grad = [&](float v, int j) {
+            const bool hit = counts && j == (int)t;
+            if (hit) p.loss[row] = s == 0.f ? __builtin_inff() : lse - v;
+            return zero ? 0.f : fs * exp_below(v, all) - (hit ? f : 0.f);
+        };
+        if (!p.dlogits) {
+            if (counts && threadIdx.x == 0) p.loss[row] = s == 0.f ? __builtin_inff() : lse - load_value(x + t);
+            continue;
         }
+        for (int at = threadIdx.x * V; at < whole; at += NT * V) {
+            Chunk<X, V> c;
+            c.load(x + at);
+            float g[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[i] = grad(c.get(i), at + i);
+            c.put(g);
+            c.store(dx + at, p.stream);
+        }
+        if (tail < p.classes) store_value(dx + tail, grad(load_value(x + tail), tail));
     }
 }
 
@@ -52,13 +179,23 @@ extern "C" int flashrnn_cross_entropy(const flashrnn_cross_entropy_desc_t* d, co
     const size_t e = type_size(d->io_dtype);
     if (!aligned_to(logits, e) || !aligned_to(dlogits, e) || !aligned_to(targets, type_size(d->index_dtype)) || !aligned_to(dloss, 4) || !aligned_to(loss, 4) || !aligned_to(lse, 4))
         return FLASHRNN_ERR_UNSUPPORTED;
+    const size_t rows = (size_t)d->rows;
+    const Problem p{logits, targets, (const float*)dloss, (float*)loss, (float*)lse, dlogits, rows, (size_t)d->logits_stride, (size_t)d->dlogits_stride, d->classes,
+                    d->index_dtype == FLASHRNN_I64, rows * d->classes * e > kStreamBytes, d->grad_scale};
+    const hipStream_t stream = (hipStream_t)hip_stream;
     return with_io_type(d->io_dtype, [&](auto* xt) {
-        return with_index_type(d->index_dtype, [&](auto* it) {
-            using X = std::remove_pointer_t<decltype(xt)>;
-            using I = std::remove_pointer_t<decltype(it)>;
-            hipLaunchKernelGGL((cross_entropy_kernel<X, I>), dim3(row_blocks((size_t)d->rows)), dim3(kThreads), 0, (hipStream_t)hip_stream, (size_t)d->rows, d->classes, (size_t)d->logits_stride,
-                               (size_t)d->dlogits_stride, (const X*)logits, (const I*)targets, (const float*)dloss, d->grad_scale, (float*)loss, (float*)lse, (X*)dlogits);
-            return launch_status();
-        });
+        using X = std::remove_pointer_t<decltype(xt)>;
+        constexpr int V = 16 / sizeof(X);
+        int rc = FLASHRNN_OK;
+        auto launch = [&](auto s) {
+            constexpr int L = decltype(s)::L, K = decltype(s)::K, NT = threads_of<L>(), PER = NT / L;
+            hipLaunchKernelGGL((loss_rows_kernel<X, L, K>), dim3(row_blocks((rows + PER - 1) / PER)), dim3(NT), 0, stream, p);
+            rc = launch_status();
+        };
+        const int chunks = (d->classes + V - 1) / V;
+        if (d->classes >= V && (with_shape(chunks, launch) || with_long_shape(chunks, launch))) return rc;
+        if (d->classes < V) hipLaunchKernelGGL((loss_long_kernel<X, kWave>), dim3(row_blocks(rows)), dim3(kWave), 0, stream, p);
+        else hipLaunchKernelGGL((loss_long_kernel<X, 1024>), dim3(row_blocks(rows)), dim3(1024), 0, stream, p);
+        return launch_status();
     });
 }

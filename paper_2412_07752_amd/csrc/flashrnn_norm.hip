@@ -5,7 +5,6 @@ using namespace flashrnn;
 
 namespace {
 
-constexpr int kThreads = 256;
 // Workgroups of a forward call: 65536 x 8 x 256 states take 161 us with 768 workgroups of 256 threads, 162 with 2048, 148 with 8192 and 160 with one row for every
 // group of threads.
 constexpr unsigned kMostThreads = 8192 * 256;
@@ -53,27 +52,8 @@ __global__ __launch_bounds__(kThreads) void layer_norm_fwd_kernel(Rows r, const 
     }
 }
 
-// Rows in registers.  A row is read once: a group of L threads (lanes of a wave, or a whole workgroup) holds it as K chunks of V values a thread, chunk
-// k of thread l being number k * L + l.  The last chunk of a row whose length is no multiple of V ends with the row and overlaps the one before it: the values that both
-// hold count once in the sums and are stored twice, the same.  Threads beyond the last chunk hold that chunk too, count nothing and store nothing.  Groups
-// take rows a fixed number apart, which is a multiple of `groups`, so that a thread's part of weight and bias stays in its registers; the next row's loads are on
-// their way while this row is worked on.
-template <int L> constexpr int threads_of() { return L <= kWave ? kThreads : L; }
-
-template <int L, int K, int V> struct RowPart {
-    int at[K];      // first value of each chunk
-    int skip;       // values at the start of chunk K - 1 that the chunk before it holds (V: all, nothing is stored)
-    __device__ __forceinline__ RowPart(int l, int width) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) at[k] = (k * L + l) * V;
-        const int last = width - V;
-        skip = at[K - 1] > last ? (at[K - 1] < width ? at[K - 1] - last : V) : 0;
-        at[K - 1] = at[K - 1] > last ? last : at[K - 1];
-    }
-    __device__ __forceinline__ bool counts(int k, int i) const { return k < K - 1 || i >= skip; }
-    __device__ __forceinline__ bool stores(int k) const { return k < K - 1 || skip < V; }
-};
-
+// Rows in registers, laid out as RowPart says, read once.  Groups take rows a fixed number apart, which is a multiple of `groups`, so that a thread's part of weight and bias
+// stays in its registers; the next row's loads are on their way while this row is worked on.
 template <typename X, int V, int L, int K>
 __global__ __launch_bounds__(threads_of<L>()) void layer_norm_rows_kernel(Rows r, const X* __restrict__ x, const void* __restrict__ weight, const void* __restrict__ bias,
                                                                          bool params_bf16, void* __restrict__ y, bool y_bf16, bool stream, float* __restrict__ mean_out,
@@ -292,20 +272,6 @@ __global__ __launch_bounds__(kSumWaves * kWave) void layer_norm_sum_strips_kerne
     }
 }
 
-// calls f(L, K) as compile-time constants: the smallest group that holds `chunks` chunks, in waves' lanes first, then workgroups; false if none does
-template <int A, int B> struct Shape { static constexpr int L = A, K = B; };
-template <typename F> bool with_shape(int chunks, F&& f) {
-    bool done = false;
-    auto take = [&](auto s) {
-        if (!done && chunks <= decltype(s)::L * decltype(s)::K) {
-            f(s);
-            done = true;
-        }
-    };
-    take(Shape<8, 1>{}); take(Shape<8, 2>{}); take(Shape<8, 3>{}); take(Shape<8, 4>{}); take(Shape<16, 3>{}); take(Shape<16, 4>{}); take(Shape<32, 3>{}); take(Shape<32, 4>{});
-    take(Shape<64, 3>{}); take(Shape<64, 4>{}); take(Shape<256, 2>{}); take(Shape<256, 3>{}); take(Shape<256, 4>{}); take(Shape<512, 3>{}); take(Shape<512, 4>{});
-    return done;
-}
 // workgroups of PER groups of threads each: at most `most`, and a number that keeps a group's rows on one row of the weights
 inline size_t lcm_of(size_t a, size_t b) {
     size_t x = a, y = b;

@@ -68,6 +68,15 @@ template <typename T, int V> struct Chunk {
             }
         }
     }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = 0;
+    }
+    // nothing computed from these words before is kept: what is needed again is formed from them again, and the registers hold the words alone
+    __device__ __forceinline__ void refresh() {
+#pragma unroll
+        for (int i = 0; i < W; ++i) asm volatile("" : "+v"(w[i]));
+    }
     __device__ __forceinline__ float get(int i) const {   // (i: known when compiled)
         if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
         else return __builtin_bit_cast(float, i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
@@ -107,43 +116,45 @@ template <int V> __device__ __forceinline__ void store_chunk(void* base, bool bf
     }
 }
 
-// sum over groups of L lanes, the same in every lane (all lanes of the wave take part)
-template <int L> __device__ __forceinline__ float lanes_sum(float v) {
+// f(f(a, b), ...) over groups of L lanes, the same in every lane (all lanes of the wave take part)
+template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, false)); }
+template <int L, typename F> __device__ __forceinline__ float lanes_fold(float v, F&& f) {
     static_assert(L == 8 || L == 16 || L == 32 || L == 64, "lanes of a wave");
-#define FLASHRNN_DPP(x, ctrl) __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, 0xF, 0xF, false))
-    v += FLASHRNN_DPP(v, 0xB1);    // lane ^ 1
-    v += FLASHRNN_DPP(v, 0x4E);    // lane ^ 2
-    v += FLASHRNN_DPP(v, 0x141);   // 7 - lane: the other four of eight
-    if constexpr (L >= 16) v += FLASHRNN_DPP(v, 0x140);   // 15 - lane
-#undef FLASHRNN_DPP
+    v = f(v, dpp<0xB1>(v));    // lane ^ 1
+    v = f(v, dpp<0x4E>(v));    // lane ^ 2
+    v = f(v, dpp<0x141>(v));   // 7 - lane: the other four of eight
+    if constexpr (L >= 16) v = f(v, dpp<0x140>(v));   // 15 - lane
     if constexpr (L >= 32) {   // rows of 16 lanes, then halves of 32, exchanged between two copies
         const uint32_t b = __builtin_bit_cast(uint32_t, v);
         const auto p = __builtin_amdgcn_permlane16_swap(b, b, false, false);
         const uint32_t x = p[0], y = p[1];
-        v = __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+        v = f(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y));
     }
     if constexpr (L >= 64) {
         const uint32_t b = __builtin_bit_cast(uint32_t, v);
         const auto p = __builtin_amdgcn_permlane32_swap(b, b, false, false);
         const uint32_t x = p[0], y = p[1];
-        v = __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+        v = f(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y));
     }
     return v;
 }
-// sum over a group of L threads: lanes of a wave, or a whole workgroup of L threads, whose waves meet in slot (two slots taken in turn need no other barrier)
-template <int L> __device__ __forceinline__ float group_sum(float v, float* slot) {
+template <int L> __device__ __forceinline__ float lanes_sum(float v) { return lanes_fold<L>(v, [](float a, float b) { return a + b; }); }
+// the same over a group of L threads: lanes of a wave, or a whole workgroup of L threads, whose waves meet in slot (two slots taken in turn need no other barrier)
+template <int L, typename F> __device__ __forceinline__ float group_fold(float v, float* slot, F&& f) {
     if constexpr (L <= kWave) {
-        return lanes_sum<L>(v);
+        return lanes_fold<L>(v, f);
     } else {
-        v = lanes_sum<kWave>(v);
+        v = lanes_fold<kWave>(v, f);
         if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
         __syncthreads();
         float s = slot[0];
 #pragma unroll
-        for (int i = 1; i < L / kWave; ++i) s += slot[i];
+        for (int i = 1; i < L / kWave; ++i) s = f(s, slot[i]);
         return s;
     }
 }
+template <int L> __device__ __forceinline__ float group_sum(float v, float* slot) { return group_fold<L>(v, slot, [](float a, float b) { return a + b; }); }
+template <int L> __device__ __forceinline__ float group_max(float v, float* slot) { return group_fold<L>(v, slot, [](float a, float b) { return fmaxf(a, b); }); }
 
 // sum over the threads of a workgroup of NT threads, the same in every thread; `lds` holds NT / 64 values
 template <int NT, typename T> __device__ __forceinline__ T block_sum(T v, T* lds) {
@@ -157,16 +168,50 @@ template <int NT, typename T> __device__ __forceinline__ T block_sum(T v, T* lds
     for (int i = 0; i < NT / kWave; ++i) s += lds[i];
     return s;
 }
-template <int NT> __device__ __forceinline__ float block_max(float v, float* lds) {
+// Rows in registers: a group of L threads (lanes of a wave, or a whole workgroup) holds a row as K chunks of V values a thread, chunk k of thread l being number
+// k * L + l.  The last chunk of a row whose length is no multiple of V ends with the row and overlaps the one before it: the values that both hold count once in sums and are
+// stored twice, the same.  Threads beyond the last chunk hold that chunk too, count nothing and store nothing.  (The K of a length is the smallest: all but the last
+// chunk of a thread are whole.)
+constexpr int kThreads = 256;
+template <int L> constexpr int threads_of() { return L <= kWave ? kThreads : L; }
+
+template <int L, int K, int V> struct RowPart {
+    int at[K];      // first value of each chunk
+    int skip;       // values at the start of chunk K - 1 that the chunk before it holds (V: all, nothing is stored)
+    __device__ __forceinline__ RowPart(int l, int width) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float s = lds[0];
-#pragma unroll
-    for (int i = 1; i < NT / kWave; ++i) s = fmaxf(s, lds[i]);
-    return s;
+        for (int k = 0; k < K; ++k) at[k] = (k * L + l) * V;
+        const int last = width - V;
+        skip = at[K - 1] > last ? (at[K - 1] < width ? at[K - 1] - last : V) : 0;
+        at[K - 1] = at[K - 1] > last ? last : at[K - 1];
+    }
+    __device__ __forceinline__ bool counts(int k, int i) const { return k < K - 1 || i >= skip; }
+    __device__ __forceinline__ bool stores(int k) const { return k < K - 1 || skip < V; }
+};
+
+// calls f(L, K) as compile-time constants: the smallest group that holds `chunks` chunks, in waves' lanes first, then workgroups; false if none does
+template <int A, int B> struct Shape { static constexpr int L = A, K = B; };
+template <typename F> bool with_shape(int chunks, F&& f) {
+    bool done = false;
+    auto take = [&](auto s) {
+        if (!done && chunks <= decltype(s)::L * decltype(s)::K) {
+            f(s);
+            done = true;
+        }
+    };
+    take(Shape<8, 1>{}); take(Shape<8, 2>{}); take(Shape<8, 3>{}); take(Shape<8, 4>{}); take(Shape<16, 3>{}); take(Shape<16, 4>{}); take(Shape<32, 3>{}); take(Shape<32, 4>{});
+    take(Shape<64, 3>{}); take(Shape<64, 4>{}); take(Shape<256, 2>{}); take(Shape<256, 3>{}); take(Shape<256, 4>{}); take(Shape<512, 3>{}); take(Shape<512, 4>{});
+    return done;
+}
+// the same for workgroups of 1024 threads
+template <int K = 3, typename F> bool with_long_shape(int chunks, F&& f) {
+    if constexpr (K > 16) {
+        return false;
+    } else {
+        if (chunks > 1024 * K) return with_long_shape<K + 1>(chunks, f);
+        f(Shape<1024, K>{});
+        return true;
+    }
 }
 
 // calls f with a null pointer of the C++ type behind a flashrnn_dtype_t / flashrnn_index_t
