@@ -246,8 +246,8 @@ typedef enum { FLASHRNN_I32 = 2, FLASHRNN_I64 = 3 } flashrnn_index_t;
  *   workspace  flashrnn_embedding_workspace_bytes() bytes, 256-byte aligned, any content (gradient only)
  */
 typedef struct {
-    long long tokens;   /* >= 0, below 2^31 for the gradient */
-    int vocab, width;   /* > 0 */
+    long long tokens;   /* >= 0, below 2^29 for the gradient */
+    int vocab, width;   /* > 0; width at most 2^23 */
     int table_dtype, io_dtype, index_dtype;
     float scale;
 } flashrnn_embedding_desc_t;

@@ -1,22 +1,28 @@
 // Embedding lookup and its gradient by sorted tokens (include/flashrnn.h).
 //
-// The gradient sorts the places by their word (stable, so that the places of a word stay in order) with a radix sort of digits of up to
-// kDigitBits bits, least significant first.  Per digit: every workgroup counts the digits of its kTile places, then every workgroup adds up
-// the counts of smaller digits and of the workgroups before it and moves its places behind them.  Tokens outside the vocabulary
-// sort behind all words.
+// The gradient sorts the places by their word, stable, so that the places of a word stay in order: a radix sort, least significant digit first, by one workgroup in its LDS up to
+// kSmall places, by tiles of places on many workgroups beyond.  The table's rows are filled with zeros by the workgroups that the sort leaves idle.  Then groups of lanes
+// add up runs of consecutive sorted places and write the rows of the words that begin and end inside; what is left of a word at the ends of a run goes to the workspace, and a last kernel joins such pieces
+// in order.  Tokens outside the vocabulary sort behind all words.
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;
 
 namespace {
 
-constexpr int kWaves = kThreads / kWave;
-constexpr int kDigitBits = 8;
+constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
-constexpr int kTile = 2048;   // places per workgroup of the sort
+constexpr int kSmall = 8192;       // places that one workgroup sorts
+constexpr int kMaxTiles = 128;     // tiles of a larger sort
+constexpr int kSortThreads = 1024;
+constexpr int kSortWaves = kSortThreads / kWave;
+constexpr int kRounds = kSmall / kSortThreads;   // places per thread of the one workgroup
+constexpr int kTileRounds = 2;                   // ... of a tile at a time
+constexpr uint32_t kMinRun = 8, kMaxRun = 64;   // sorted places that a group of lanes adds up
+constexpr int kFillBlocks = 2048;
 
-template <typename I> __device__ __forceinline__ uint32_t key_of(const I* tokens, size_t i, uint32_t vocab) {
-    const int64_t t = tokens[i];
+__device__ __forceinline__ uint32_t key_of(const void* tokens, bool index64, size_t i, uint32_t vocab) {
+    const int64_t t = index64 ? ((const int64_t*)tokens)[i] : ((const int32_t*)tokens)[i];
     return t >= 0 && t < (int64_t)vocab ? (uint32_t)t : vocab;
 }
 
@@ -29,154 +35,415 @@ __global__ __launch_bounds__(kThreads) void embedding_fwd_kernel(size_t n, int v
     }
 }
 
-// counts[digit][workgroup]; keys == nullptr: the first digit, straight from the tokens
-template <typename I>
-__global__ __launch_bounds__(kThreads) void count_digits_kernel(const I* __restrict__ tokens, const uint32_t* __restrict__ keys, size_t n, uint32_t vocab, int shift,
-                                                                uint32_t* __restrict__ counts) {
-    __shared__ uint32_t lds[kDigits];
-    for (int d = threadIdx.x; d < kDigits; d += kThreads) lds[d] = 0;
-    __syncthreads();
-    for (int u = threadIdx.x; u < kTile; u += kThreads) {
-        const size_t i = (size_t)blockIdx.x * kTile + u;
-        if (i < n) atomicAdd(&lds[(keys ? keys[i] : key_of(tokens, i, vocab)) >> shift & (kDigits - 1)], 1u);   // (whole numbers: any order)
-    }
-    __syncthreads();
-    for (int d = threadIdx.x; d < kDigits; d += kThreads) counts[(size_t)d * gridDim.x + blockIdx.x] = lds[d];
-}
-
-// exclusive sums over counts[digit][workgroup], by one workgroup
-__global__ __launch_bounds__(1024) void scan_counts_kernel(uint32_t* __restrict__ counts, size_t n) {
-    __shared__ uint32_t lds[1024];
-    uint32_t before = 0;
-    for (size_t at = 0; at < n; at += 1024) {
-        const size_t i = at + threadIdx.x;
-        const uint32_t v = i < n ? counts[i] : 0;
-        lds[threadIdx.x] = v;
-        __syncthreads();
-        for (int o = 1; o < 1024; o <<= 1) {
-            const uint32_t a = threadIdx.x >= (unsigned)o ? lds[threadIdx.x - o] : 0;
-            __syncthreads();
-            lds[threadIdx.x] += a;
-            __syncthreads();
-        }
-        if (i < n) counts[i] = before + lds[threadIdx.x] - v;
-        before += lds[1023];
-        __syncthreads();
+// zeros for floats [begin, end) of the table, by workgroups 0 .. blocks - 1 of NT threads
+struct Fill {
+    float* table;
+    size_t begin, end;
+};
+template <int NT> __device__ __forceinline__ void fill_zeros(const Fill& f, unsigned block, unsigned blocks) {
+    Chunk<float, 4> zero;
+    zero.clear();
+    for (size_t i = f.begin + ((size_t)block * NT + threadIdx.x) * 4; i < f.end; i += (size_t)blocks * NT * 4) {
+        if (i + 4 <= f.end) zero.store(f.table + i, true);
+        else
+            for (size_t j = i; j < f.end; ++j) f.table[j] = 0.f;
     }
 }
 
-// A wave takes the 64 places of a run in order: lanes with the same digit find each other by comparing the digits' bits, and the lane's place
-// among them is the number of lower lanes.  Waves take runs of their own behind one another: wave w the runs w * kRuns, ...
-template <typename I>
-__global__ __launch_bounds__(kThreads) void move_places_kernel(const I* __restrict__ tokens, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ places, size_t n,
-                                                               uint32_t vocab, int shift, const uint32_t* __restrict__ offsets, uint32_t* __restrict__ keys_out,
-                                                               uint32_t* __restrict__ places_out) {
-    constexpr int kRuns = kTile / kThreads;
-    __shared__ uint32_t lds[kWaves][kDigits];
+// Digits of 64 places a wave at a time: lanes with the same digit find each other by comparing the digits' bits; a lane's rank is the number of lower lanes with its
+// digit behind those that the wave has counted before.  count: the wave's own row of kDigits counters.
+__device__ __forceinline__ uint32_t rank_in_wave(uint32_t digit, bool in, int bits, uint32_t* count) {
+    uint64_t same = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t m = __ballot(digit >> b & 1);
+        same &= digit >> b & 1 ? m : ~m;
+    }
+    const int lane = threadIdx.x & 63;
+    const uint32_t lower = __popcll(same & ((1ull << lane) - 1));
+    const uint32_t base = in ? count[digit] : 0;   // (one wave, one row: its LDS accesses are in order)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (in && lower == 0) count[digit] = base + __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    return base + lower;
+}
+// exclusive sums over the first kDigits threads of the workgroup
+__device__ __forceinline__ uint32_t scan_digits(uint32_t v, uint32_t* lds) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    for (int d = threadIdx.x; d < kWaves * kDigits; d += kThreads) lds[0][d] = 0;
-    __syncthreads();
-    uint32_t key[kRuns], rank[kRuns];
+    uint32_t s = v;
 #pragma unroll
-    for (int u = 0; u < kRuns; ++u) {
-        const size_t i = (size_t)blockIdx.x * kTile + (w * kRuns + u) * kWave + lane;
-        const bool in = i < n;
-        key[u] = in ? (keys ? keys[i] : key_of(tokens, i, vocab)) : 0;
-        const uint32_t d = key[u] >> shift & (kDigits - 1);
-        uint64_t same = __ballot(in);
-#pragma unroll
-        for (int b = 0; b < kDigitBits; ++b) {
-            const uint64_t m = __ballot(d >> b & 1);
-            same &= d >> b & 1 ? m : ~m;
-        }
-        const uint32_t lower = __popcll(same & ((1ull << lane) - 1));
-        const uint32_t base = lds[w][d];   // (one wave, one row: its LDS accesses are in order)
-        rank[u] = base + lower;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (in && lower == 0) lds[w][d] = base + __popcll(same);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int o = 1; o < kWave; o <<= 1) {
+        const uint32_t a = __shfl_up(s, o);
+        if (lane >= o) s += a;
     }
+    if (w < kDigits / kWave && lane == 63) lds[w] = s;
     __syncthreads();
-    for (int d = threadIdx.x; d < kDigits; d += kThreads) {
-        uint32_t at = offsets[(size_t)d * gridDim.x + blockIdx.x];
+    uint32_t before = 0;
+    for (int i = 0; i < w && i < kDigits / kWave; ++i) before += lds[i];
+    return before + s - v;
+}
+
+// up to kSmall places, sorted by workgroup 0; the others fill
+__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const void* __restrict__ tokens, bool index64, uint32_t n, uint32_t vocab, int passes, int bits,
+                                                                  uint32_t* __restrict__ keys_out, uint32_t* __restrict__ places_out, Fill fill) {
+    __shared__ uint32_t keys[kSmall], counts[kSortWaves][kDigits], totals[kDigits / kWave];
+    __shared__ uint16_t places[kSmall];
+    if (blockIdx.x) return fill_zeros<kSortThreads>(fill, blockIdx.x - 1, gridDim.x - 1);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint32_t runs = (n + kWave - 1) / kWave, mine = (runs + kSortWaves - 1) / kSortWaves;   // runs of 64 places, `mine` of them in a row a wave
+    uint32_t key[kRounds], rank[kRounds];
+    uint16_t place[kRounds];
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
-            const uint32_t c = lds[v][d];
-            lds[v][d] = at;
-            at += c;
+    for (int u = 0; u < kRounds; ++u) {
+        const uint32_t i = (w * mine + u) * kWave + lane;
+        const bool in = (uint32_t)u < mine && i < n;
+        key[u] = in ? key_of(tokens, index64, i, vocab) : ~0u;
+        place[u] = (uint16_t)i;
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * bits;
+        const uint32_t mask = (1u << bits) - 1;
+        for (int d = threadIdx.x; d < kSortWaves * kDigits; d += kSortThreads) counts[0][d] = 0;
+        __syncthreads();   // (and every wave has read the last pass's keys)
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u)
+            if ((uint32_t)u < mine) rank[u] = rank_in_wave(key[u] >> shift & mask, key[u] != ~0u, bits, counts[w]);
+        __syncthreads();
+        uint32_t total = 0;
+        if (threadIdx.x < kDigits)
+            for (int v = 0; v < kSortWaves; ++v) {
+                const uint32_t c = counts[v][threadIdx.x];
+                counts[v][threadIdx.x] = total;
+                total += c;
+            }
+        const uint32_t before = scan_digits(total, totals);
+        if (threadIdx.x < kDigits)
+            for (int v = 0; v < kSortWaves; ++v) counts[v][threadIdx.x] += before;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u)
+            if ((uint32_t)u < mine && key[u] != ~0u) {
+                const uint32_t to = counts[w][key[u] >> shift & mask] + rank[u];
+                keys[to] = key[u];
+                places[to] = place[u];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u) {
+            const uint32_t i = (w * mine + u) * kWave + lane;
+            if ((uint32_t)u < mine && i < n) {
+                key[u] = keys[i];
+                place[u] = places[i];
+            }
         }
     }
-    __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kRuns; ++u) {
-        const size_t i = (size_t)blockIdx.x * kTile + (w * kRuns + u) * kWave + lane;
-        if (i >= n) continue;
-        const uint32_t to = lds[w][key[u] >> shift & (kDigits - 1)] + rank[u];
-        keys_out[to] = key[u];
-        places_out[to] = places ? places[i] : (uint32_t)i;
+    for (int u = 0; u < kRounds; ++u) {
+        const uint32_t i = (w * mine + u) * kWave + lane;
+        if ((uint32_t)u < mine && i < n) {
+            keys_out[i] = key[u];
+            places_out[i] = place[u];
+        }
     }
 }
 
-// the first sorted place whose word is v or a later one
-__device__ __forceinline__ size_t first_of(const uint32_t* keys, size_t n, uint32_t v) {
-    size_t lo = 0, hi = n;
-    while (lo < hi) {
-        const size_t mid = (lo + hi) / 2;
-        if (keys[mid] < v) lo = mid + 1; else hi = mid;
-    }
-    return lo;
+// One pass over more places: workgroup `tile` of `tiles` takes `span` of them.  keys == nullptr: the first digit, straight from the tokens.
+struct Pass {
+    const void* tokens;
+    const uint32_t *keys, *places;
+    uint32_t *keys_out, *places_out, *counts;   // counts[tile][digit]
+    uint32_t n, span, tiles, vocab;
+    int shift, bits, index64;
+};
+__device__ __forceinline__ uint32_t key_at(const Pass& p, uint32_t i) { return p.keys ? p.keys[i] : key_of(p.tokens, p.index64, i, p.vocab); }
+
+__global__ __launch_bounds__(kSortThreads) void count_digits_kernel(Pass p, Fill fill) {
+    __shared__ uint32_t lds[kDigits];
+    if (blockIdx.x >= p.tiles) return fill_zeros<kSortThreads>(fill, blockIdx.x - p.tiles, gridDim.x - p.tiles);
+    const uint32_t mask = (1u << p.bits) - 1;
+    if (threadIdx.x < kDigits) lds[threadIdx.x] = 0;
+    __syncthreads();
+    const uint64_t begin = (uint64_t)blockIdx.x * p.span, end = begin + p.span < p.n ? begin + p.span : p.n;
+    for (uint64_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&lds[key_at(p, (uint32_t)i) >> p.shift & mask], 1u);   // (whole numbers: any order)
+    __syncthreads();
+    if (threadIdx.x < kDigits) p.counts[(size_t)blockIdx.x * kDigits + threadIdx.x] = lds[threadIdx.x];
 }
 
-template <typename O>
-__global__ __launch_bounds__(kThreads) void sum_places_kernel(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ places, size_t n, int vocab, int width, const O* __restrict__ dout,
-                                                              float* __restrict__ dtable, float scale, int accumulate) {
-    for (uint32_t v = blockIdx.x; v < (uint32_t)vocab; v += gridDim.x) {
-        const size_t begin = first_of(keys, n, v), end = first_of(keys, n, v + 1);
-        if (begin == end && accumulate) continue;
-        for (int j = threadIdx.x; j < width; j += kThreads) {
-            float s = 0.f;
-            for (size_t p = begin; p < end; ++p) s += load_value(dout + (size_t)places[p] * width + j);
-            s *= scale;
-            float* out = dtable + (size_t)v * width + j;
-            *out = accumulate ? *out + s : s;
+__global__ __launch_bounds__(kSortThreads) void move_places_kernel(Pass p, Fill fill) {
+    __shared__ uint32_t counts[kSortWaves][kDigits], next[kDigits], totals[kDigits / kWave];
+    if (blockIdx.x >= p.tiles) return fill_zeros<kSortThreads>(fill, blockIdx.x - p.tiles, gridDim.x - p.tiles);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint32_t mask = (1u << p.bits) - 1;
+    // where this tile's places of each digit go: behind all smaller digits, and the same one in the tiles before
+    uint32_t total = 0, mine = 0;
+    if (threadIdx.x < kDigits)
+        for (uint32_t t = 0; t < p.tiles; ++t) {
+            const uint32_t c = p.counts[(size_t)t * kDigits + threadIdx.x];
+            mine += t < blockIdx.x ? c : 0;
+            total += c;
+        }
+    const uint32_t before = scan_digits(total, totals);
+    if (threadIdx.x < kDigits) next[threadIdx.x] = before + mine;
+    const uint64_t begin = (uint64_t)blockIdx.x * p.span, end = begin + p.span < p.n ? begin + p.span : p.n;
+    for (uint64_t at = begin; at < end; at += kSortThreads * kTileRounds) {
+        for (int d = threadIdx.x; d < kSortWaves * kDigits; d += kSortThreads) counts[0][d] = 0;
+        __syncthreads();
+        uint32_t key[kTileRounds], rank[kTileRounds], place[kTileRounds];
+#pragma unroll
+        for (int u = 0; u < kTileRounds; ++u) {
+            const uint64_t i = at + (w * kTileRounds + u) * kWave + lane;
+            const bool in = i < end;
+            key[u] = in ? key_at(p, (uint32_t)i) : ~0u;
+            place[u] = in && p.places ? p.places[i] : (uint32_t)i;
+        }
+#pragma unroll
+        for (int u = 0; u < kTileRounds; ++u) rank[u] = rank_in_wave(key[u] >> p.shift & mask, key[u] != ~0u, p.bits, counts[w]);
+        __syncthreads();
+        if (threadIdx.x < kDigits) {
+            uint32_t to = next[threadIdx.x];
+            for (int v = 0; v < kSortWaves; ++v) {
+                const uint32_t c = counts[v][threadIdx.x];
+                counts[v][threadIdx.x] = to;
+                to += c;
+            }
+            next[threadIdx.x] = to;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kTileRounds; ++u)
+            if (key[u] != ~0u) {
+                const uint32_t to = counts[w][key[u] >> p.shift & mask] + rank[u];
+                p.keys_out[to] = key[u];
+                p.places_out[to] = place[u];
+            }
+        __syncthreads();
+    }
+}
+
+// Groups of L lanes add up runs of `run` sorted places, V columns a lane; blockIdx.y: the block of L * V columns.  A word whose places all lie in the run is written to the table; the
+// piece of a word that began in an earlier run goes to pieces[run][0], that of one that begins here and goes on to pieces[run][1].
+struct Sum {
+    const uint32_t *keys, *places;
+    const void* dout;
+    float *table, *pieces;
+    uint32_t n, vocab, run;
+    int width, accumulate;
+    float scale;
+};
+// A lane's columns: V of them from `at` on; the last ones of a row whose length is no multiple of V overlap the lane's before, by `skip` columns (V: another lane has them all).  Rows
+// shorter than V: one lane has them, value by value.
+template <int V> struct Columns {
+    int at, skip, narrow;
+    __device__ __forceinline__ Columns(int chunk, int width) {
+        const int last = width - V;
+        narrow = last < 0 ? width : 0;
+        at = narrow ? 0 : chunk * V > last ? last : chunk * V;
+        skip = narrow ? (chunk ? V : 0) : chunk * V >= width ? V : chunk * V - at;
+    }
+    template <typename T> __device__ __forceinline__ Chunk<T, V> load(const T* row) const {
+        Chunk<T, V> c;
+        if (!narrow) {
+            c.load(row + at);
+        } else {
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = i < narrow ? load_value(row + i) : 0.f;
+            c.put(v);
+        }
+        return c;
+    }
+    template <typename T> __device__ __forceinline__ void store(T* row, const float (&v)[V]) const {
+        if (skip == V) return;
+        if (!narrow) {
+            Chunk<T, V> c;
+            c.put(v);
+            c.store(row + at);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < narrow) store_value(row + i, v[i]);
         }
     }
+    // row += v: a column that two lanes hold is one's alone
+    __device__ __forceinline__ void add(float* row, float (&v)[V]) const {
+        if (skip == V) return;
+        if (!skip && !narrow) {
+            Chunk<float, V> c;
+            c.load(row + at);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += c.get(i);
+            c.put(v);
+            c.store(row + at);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i >= skip && (!narrow || i < narrow)) row[at + i] += v[i];
+        }
+    }
+};
+template <int V> __device__ __forceinline__ void put_row(const Sum& q, const Columns<V>& c, uint32_t word, float (&s)[V]) {
+    float* row = q.table + (size_t)word * q.width;
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] *= q.scale;
+    if (q.accumulate) c.add(row, s);
+    else c.store(row, s);
 }
 
-int check_desc(const flashrnn_embedding_desc_t* d) {
+template <typename O, int L>
+__global__ __launch_bounds__(kThreads) void sum_runs_kernel(Sum q) {
+    constexpr int V = 16 / sizeof(O), kAhead = 8;
+    const uint32_t r = blockIdx.x * (kThreads / L) + threadIdx.x / L;
+    const uint64_t begin = (uint64_t)r * q.run;
+    if (begin >= q.n) return;
+    const uint32_t b = (uint32_t)begin, e = q.n - b < q.run ? q.n : b + q.run;
+    const Columns<V> col(blockIdx.y * L + threadIdx.x % L, q.width);
+    float* pieces = q.pieces + (size_t)r * 2 * q.width;
+    const uint32_t before = b ? q.keys[b - 1] : ~0u;
+    uint32_t word = q.keys[b];
+    float s[V] = {};
+    for (uint32_t p = b; p < e && word < q.vocab; p += kAhead) {
+        uint32_t key[kAhead];
+        Chunk<O, V> row[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t at = p + u < e ? p + u : e - 1;
+            key[u] = q.keys[at];
+            row[u] = col.load((const O*)q.dout + (size_t)q.places[at] * q.width);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (p + u >= e) break;
+            if (key[u] != word) {
+                if (word == before) col.store(pieces, s);
+                else put_row(q, col, word, s);
+                word = key[u];
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[i] = 0.f;
+                if (word == q.vocab) break;
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[i] += row[u].get(i);
+        }
+    }
+    if (word == q.vocab) return;
+    if (word == before) col.store(pieces, s);
+    else if (e < q.n && q.keys[e] == word) col.store(pieces + q.width, s);
+    else put_row(q, col, word, s);
+}
+
+// A workgroup per run (and 256 columns): where a word begins in the run and goes on beyond it, its pieces are added up, every kJoinWaves-th by a wave, and its row is written.
+constexpr int kJoinWaves = 4;
+__global__ __launch_bounds__(kJoinWaves * kWave) void join_pieces_kernel(Sum q, uint32_t runs) {
+    constexpr int V = 4, kAhead = 4;
+    __shared__ float lds[kJoinWaves][kWave][V];
+    const uint32_t r = blockIdx.x, b = r * q.run, e = q.n - b < q.run ? q.n : b + q.run;
+    if (e == q.n) return;
+    const uint32_t word = q.keys[e - 1];
+    if (word == q.vocab || q.keys[e] != word || (b && q.keys[b - 1] == word)) return;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    uint32_t more = 0;   // runs that the word goes on through: those that begin with it
+    while (true) {
+        const uint64_t next = (uint64_t)r + 1 + more + lane;
+        const uint64_t m = __ballot(next < runs && q.keys[next < runs ? next * q.run : 0] == word);
+        if (~m) {
+            more += __builtin_ctzll(~m);
+            break;
+        }
+        more += kWave;
+    }
+    const Columns<V> col(blockIdx.y * kWave + lane, q.width);
+    const size_t step = 2 * (size_t)q.width;
+    const float* from = q.pieces + (size_t)r * step;
+    float s[V] = {};
+    if (w == 0) {
+        const Chunk<float, V> c = col.load(from + q.width);
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] = c.get(i);
+    }
+    for (uint32_t k = 1 + w; k <= more; k += kAhead * kJoinWaves) {
+        Chunk<float, V> c[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t at = k + u * kJoinWaves <= more ? k + u * kJoinWaves : more;
+            c[u] = col.load(from + at * step);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (k + u * kJoinWaves <= more)
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[i] += c[u].get(i);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) lds[w][lane][i] = s[i];
+    __syncthreads();
+    if (w) return;
+    for (int v = 1; v < kJoinWaves; ++v)
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] += lds[v][lane][i];
+    put_row(q, col, word, s);
+}
+
+int check_desc(const flashrnn_embedding_desc_t* d, bool gradient) {
     if (!d) return FLASHRNN_ERR_NULL;
     if (d->tokens < 0 || d->vocab <= 0 || d->width <= 0) return FLASHRNN_ERR_SHAPE;
     if (!is_io_type(d->table_dtype) || !is_io_type(d->io_dtype) || !is_index_type(d->index_dtype)) return FLASHRNN_ERR_SHAPE;
-    if (d->tokens > 2147483647LL) return FLASHRNN_ERR_UNSUPPORTED;
+    // every offset below 2^62 bytes; the gradient's workgroups (one per run of places, and so on) below 2^32 threads, 2^16 in the other direction
+    if ((double)d->tokens * d->width > 1e18 || d->width > (1 << 23) || (gradient && d->tokens >= (1LL << 29))) return FLASHRNN_ERR_UNSUPPORTED;
     return FLASHRNN_OK;
 }
 
-struct Workspace {
-    size_t tiles, keys[2], places[2], counts, total;
+// How the gradient is laid out: the sort's passes and tiles, the runs, the workspace.
+struct Plan {
+    int passes, bits;
+    uint32_t tiles, span;   // tiles = 0: the sort of one workgroup
+    int L, blocks_y;
+    uint32_t run, runs;
+    size_t keys[2], places[2], counts, pieces, total;
 };
-Workspace workspace_of(const flashrnn_embedding_desc_t* d) {
+Plan plan_of(const flashrnn_embedding_desc_t* d) {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-    Workspace w;
-    const size_t list = up((size_t)d->tokens * 4);
-    w.tiles = ((size_t)d->tokens + kTile - 1) / kTile;
-    size_t at = 0;
-    for (int i = 0; i < 2; ++i) {
-        w.keys[i] = at; at += list;
-        w.places[i] = at; at += list;
+    Plan p;
+    const size_t n = (size_t)d->tokens;
+    int bits = 1;
+    while ((uint64_t)d->vocab >> bits) ++bits;   // keys go up to vocab itself
+    p.passes = (bits + kDigitBits - 1) / kDigitBits;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    p.tiles = p.span = 0;
+    if (n > kSmall) {
+        const size_t step = kSortThreads * kTileRounds, steps = (n + step - 1) / step, each = (steps + kMaxTiles - 1) / kMaxTiles;
+        p.span = (uint32_t)(each * step);
+        p.tiles = (uint32_t)((n + p.span - 1) / p.span);
     }
-    w.counts = at;
-    w.total = at + up(w.tiles * kDigits * 4) + 256;
-    return w;
+    // lanes per row: the number that leaves the fewest of them without columns, the larger one of equals
+    const int V = 16 / (int)type_size(d->io_dtype), chunks = (d->width + V - 1) / V;
+    p.L = 64;
+    for (int L = 32; L >= 8; L /= 2)
+        if ((chunks + L - 1) / L * L < (chunks + p.L - 1) / p.L * p.L) p.L = L;
+    p.blocks_y = (chunks + p.L - 1) / p.L;
+    // places per run: enough runs for 2048 waves, as long as that leaves them kMinRun places or more
+    const size_t waves = n * p.blocks_y * p.L / kWave;
+    p.run = kMaxRun;
+    while (p.run > kMinRun && waves / p.run < 2048) p.run /= 2;
+    p.runs = (uint32_t)((n + p.run - 1) / p.run);
+    size_t at = 0;
+    const size_t list = up(n * 4);
+    for (int i = 0; i < 2; ++i) {
+        p.keys[i] = at; at += list;
+        p.places[i] = at; at += list;
+    }
+    p.counts = at; at += up((size_t)p.tiles * kDigits * 4);
+    p.pieces = at; at += up((size_t)p.runs * 2 * d->width * 4);
+    p.total = at + 256;
+    return p;
 }
 
 }  // namespace
 
 extern "C" {
 
-size_t flashrnn_embedding_workspace_bytes(const flashrnn_embedding_desc_t* d) { return check_desc(d) == FLASHRNN_OK ? workspace_of(d).total : 0; }
+size_t flashrnn_embedding_workspace_bytes(const flashrnn_embedding_desc_t* d) { return check_desc(d, true) == FLASHRNN_OK ? plan_of(d).total : 0; }
 
 int flashrnn_embedding_fwd(const flashrnn_embedding_desc_t* d, const void* table, const void* tokens, void* out, void* hip_stream) {
-    const int rc = check_desc(d);
+    const int rc = check_desc(d, false);
     if (rc != FLASHRNN_OK) return rc;
     if (d->tokens == 0) return FLASHRNN_OK;
     if (!table || !tokens || !out) return FLASHRNN_ERR_NULL;
@@ -196,43 +463,59 @@ int flashrnn_embedding_fwd(const flashrnn_embedding_desc_t* d, const void* table
 }
 
 int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* tokens, const void* dout, void* dtable, int accumulate, void* workspace, void* hip_stream) {
-    const int rc = check_desc(d);
+    const int rc = check_desc(d, true);
     if (rc != FLASHRNN_OK) return rc;
     const size_t n = (size_t)d->tokens;
     if (!dtable || (n && (!tokens || !dout))) return FLASHRNN_ERR_NULL;
     if (!workspace || !aligned_to(workspace, 256)) return FLASHRNN_ERR_WORKSPACE;
     if (!aligned_to(dout, type_size(d->io_dtype)) || !aligned_to(tokens, type_size(d->index_dtype)) || !aligned_to(dtable, 4)) return FLASHRNN_ERR_UNSUPPORTED;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const Workspace w = workspace_of(d);
+    const Plan p = plan_of(d);
     char* ws = (char*)workspace;
-    uint32_t *keys = nullptr, *places = nullptr, *counts = (uint32_t*)(ws + w.counts);
-    const unsigned tiles = (unsigned)w.tiles;
-    if (n) {
-        int bits = 0;
-        while (bits < 32 && (uint64_t)d->vocab >> bits) ++bits;   // keys go up to vocab itself
-        for (int shift = 0, pass = 0; shift < bits; shift += kDigitBits, ++pass) {
-            uint32_t *keys_to = (uint32_t*)(ws + w.keys[pass & 1]), *places_to = (uint32_t*)(ws + w.places[pass & 1]);
-            const int e = with_index_type(d->index_dtype, [&](auto* it) {
-                using I = std::remove_pointer_t<decltype(it)>;
-                hipLaunchKernelGGL((count_digits_kernel<I>), dim3(tiles), dim3(kThreads), 0, stream, (const I*)tokens, (const uint32_t*)keys, n, (uint32_t)d->vocab, shift, counts);
-                if (const int err = launch_status()) return err;
-                hipLaunchKernelGGL(scan_counts_kernel, dim3(1), dim3(1024), 0, stream, counts, (size_t)tiles * kDigits);
-                if (const int err = launch_status()) return err;
-                hipLaunchKernelGGL((move_places_kernel<I>), dim3(tiles), dim3(kThreads), 0, stream, (const I*)tokens, (const uint32_t*)keys, (const uint32_t*)places, n,
-                                   (uint32_t)d->vocab, shift, (const uint32_t*)counts, keys_to, places_to);
-                return launch_status();
-            });
-            if (e != FLASHRNN_OK) return e;
-            keys = keys_to;
-            places = places_to;
+    const size_t floats = accumulate ? 0 : (size_t)d->vocab * d->width;
+    const size_t per_block = kSortThreads * 4 * 4;   // floats that a workgroup fills at least
+    auto fill_blocks = [&](const Fill& f) { return (unsigned)((f.end - f.begin + per_block - 1) / per_block < kFillBlocks ? (f.end - f.begin + per_block - 1) / per_block : kFillBlocks); };
+    uint32_t *keys = (uint32_t*)(ws + p.keys[0]), *places = (uint32_t*)(ws + p.places[0]);
+    if (p.tiles == 0) {
+        const Fill fill{(float*)dtable, 0, floats};
+        hipLaunchKernelGGL(sort_small_kernel, dim3(1 + fill_blocks(fill)), dim3(kSortThreads), 0, stream, tokens, d->index_dtype == FLASHRNN_I64, (uint32_t)n, (uint32_t)d->vocab,
+                           p.passes, p.bits, keys, places, fill);
+        if (const int e = launch_status()) return e;
+        if (n == 0) return FLASHRNN_OK;
+    } else {
+        const size_t share = (floats / (2 * p.passes) + 3) / 4 * 4;   // of the table, that one launch of the sort fills
+        size_t filled = 0;
+        Pass q{tokens, nullptr, nullptr, nullptr, nullptr, (uint32_t*)(ws + p.counts), (uint32_t)n, p.span, p.tiles, (uint32_t)d->vocab, 0, p.bits, d->index_dtype == FLASHRNN_I64};
+        for (int pass = 0; pass < p.passes; ++pass) {
+            q.shift = pass * p.bits;
+            q.keys_out = keys = (uint32_t*)(ws + p.keys[pass & 1]);
+            q.places_out = places = (uint32_t*)(ws + p.places[pass & 1]);
+            for (int step = 0; step < 2; ++step) {
+                const bool last = step == 1 && pass == p.passes - 1;
+                const Fill fill{(float*)dtable, filled, last || filled + share > floats ? floats : filled + share};
+                filled = fill.end;
+                const dim3 grid(p.tiles + fill_blocks(fill));
+                if (step == 0) hipLaunchKernelGGL(count_digits_kernel, grid, dim3(kSortThreads), 0, stream, q, fill);
+                else hipLaunchKernelGGL(move_places_kernel, grid, dim3(kSortThreads), 0, stream, q, fill);
+                if (const int e = launch_status()) return e;
+            }
+            q.keys = keys;
+            q.places = places;
         }
     }
-    return with_io_type(d->io_dtype, [&](auto* ot) {
+    const Sum q{keys, places, dout, (float*)dtable, (float*)(ws + p.pieces), (uint32_t)n, (uint32_t)d->vocab, p.run, d->width, accumulate, d->scale};
+    const int e = with_io_type(d->io_dtype, [&](auto* ot) {
         using O = std::remove_pointer_t<decltype(ot)>;
-        hipLaunchKernelGGL((sum_places_kernel<O>), dim3(row_blocks((size_t)d->vocab)), dim3(kThreads), 0, stream, (const uint32_t*)keys, (const uint32_t*)places, n, d->vocab, d->width, (const O*)dout,
-                           (float*)dtable, d->scale, accumulate);
+        const dim3 grid((p.runs + kThreads / p.L - 1) / (kThreads / p.L), p.blocks_y);
+        if (p.L == 64) hipLaunchKernelGGL((sum_runs_kernel<O, 64>), grid, dim3(kThreads), 0, stream, q);
+        else if (p.L == 32) hipLaunchKernelGGL((sum_runs_kernel<O, 32>), grid, dim3(kThreads), 0, stream, q);
+        else if (p.L == 16) hipLaunchKernelGGL((sum_runs_kernel<O, 16>), grid, dim3(kThreads), 0, stream, q);
+        else hipLaunchKernelGGL((sum_runs_kernel<O, 8>), grid, dim3(kThreads), 0, stream, q);
         return launch_status();
     });
+    if (e != FLASHRNN_OK || p.runs == 1) return e;
+    hipLaunchKernelGGL(join_pieces_kernel, dim3(p.runs, (d->width + 4 * kWave - 1) / (4 * kWave)), dim3(kJoinWaves * kWave), 0, stream, q, p.runs);
+    return launch_status();
 }
 
 }  // extern "C"
