@@ -18,8 +18,11 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / kWave;
 constexpr int kRounds = kSmall / kSortThreads;   // places per thread of the one workgroup
 constexpr int kTileRounds = 2;                   // ... of a tile at a time
+constexpr int kColumns = 4;        // columns a lane adds up: neighbours store whole cache lines of float32 (with eight, each store left every second 16 bytes out)
 constexpr uint32_t kMinRun = 8, kMaxRun = 64;   // sorted places that a group of lanes adds up
-constexpr int kFillBlocks = 2048;
+constexpr size_t kFillBlocks = 2048, kFillBytes = 8 << 10;   // workgroups that fill, at most; bytes of the table that a wave fills at a time
+constexpr size_t kFillBesideSort = 64 << 20;                  // bytes of the table that are filled beside one launch of a sort of tiles
+constexpr size_t kFlagsPerBlock = 16 << 10;
 
 __device__ __forceinline__ uint32_t key_of(const void* tokens, bool index64, size_t i, uint32_t vocab) {
     const int64_t t = index64 ? ((const int64_t*)tokens)[i] : ((const int32_t*)tokens)[i];
@@ -35,18 +38,36 @@ __global__ __launch_bounds__(kThreads) void embedding_fwd_kernel(size_t n, int v
     }
 }
 
-// zeros for floats [begin, end) of the table, by workgroups 0 .. blocks - 1 of NT threads
+// zeros for rows [begin, end) of the table, `each` (up to 64) at a time a wave: all of them, or those whose flag is not set, neighbours in one go
 struct Fill {
     float* table;
-    size_t begin, end;
+    const uint8_t* flags;
+    uint32_t begin, end, each;
+    int width;
 };
 template <int NT> __device__ __forceinline__ void fill_zeros(const Fill& f, unsigned block, unsigned blocks) {
+    constexpr int kWaves = NT / kWave;
+    const int lane = threadIdx.x & 63;
     Chunk<float, 4> zero;
     zero.clear();
-    for (size_t i = f.begin + ((size_t)block * NT + threadIdx.x) * 4; i < f.end; i += (size_t)blocks * NT * 4) {
-        if (i + 4 <= f.end) zero.store(f.table + i, true);
-        else
-            for (size_t j = i; j < f.end; ++j) f.table[j] = 0.f;
+    for (uint64_t first = f.begin + ((uint64_t)block * kWaves + threadIdx.x / kWave) * f.each; first < f.end; first += (uint64_t)blocks * kWaves * f.each) {
+        const uint64_t row = first + lane;
+        const bool in = (uint32_t)lane < f.each && row < f.end;
+        uint64_t absent = __ballot(in && (!f.flags || !f.flags[row]));
+        while (absent) {
+            const int from = __builtin_ctzll(absent);
+            const uint64_t rest = ~(absent >> from);
+            const int count = rest ? __builtin_ctzll(rest) : kWave;
+            float* at = f.table + (first + from) * f.width;
+            const uint64_t n = (uint64_t)count * f.width;
+            if (n < 4) {
+                if ((uint32_t)lane < n) at[lane] = 0.f;
+            } else {
+                for (uint64_t i = (uint64_t)lane * 4; i < n; i += 4 * kWave) zero.store(at + (i + 4 <= n ? i : n - 4), true);
+            }
+            if (from + count >= kWave) break;
+            absent &= ~0ull << (from + count);
+        }
     }
 }
 
@@ -151,6 +172,7 @@ struct Pass {
     const void* tokens;
     const uint32_t *keys, *places;
     uint32_t *keys_out, *places_out, *counts;   // counts[tile][digit]
+    uint8_t* flags;                             // of the words: cleared where the first digit is counted, set where its places are moved
     uint32_t n, span, tiles, vocab;
     int shift, bits, index64;
 };
@@ -158,7 +180,11 @@ __device__ __forceinline__ uint32_t key_at(const Pass& p, uint32_t i) { return p
 
 __global__ __launch_bounds__(kSortThreads) void count_digits_kernel(Pass p, Fill fill) {
     __shared__ uint32_t lds[kDigits];
-    if (blockIdx.x >= p.tiles) return fill_zeros<kSortThreads>(fill, blockIdx.x - p.tiles, gridDim.x - p.tiles);
+    if (blockIdx.x >= p.tiles) {
+        if (p.flags && !p.keys)
+            for (uint64_t i = (uint64_t)(blockIdx.x - p.tiles) * kSortThreads + threadIdx.x; i <= p.vocab; i += (uint64_t)(gridDim.x - p.tiles) * kSortThreads) p.flags[i] = 0;
+        return fill_zeros<kSortThreads>(fill, blockIdx.x - p.tiles, gridDim.x - p.tiles);
+    }
     const uint32_t mask = (1u << p.bits) - 1;
     if (threadIdx.x < kDigits) lds[threadIdx.x] = 0;
     __syncthreads();
@@ -176,10 +202,15 @@ __global__ __launch_bounds__(kSortThreads) void move_places_kernel(Pass p, Fill 
     // where this tile's places of each digit go: behind all smaller digits, and the same one in the tiles before
     uint32_t total = 0, mine = 0;
     if (threadIdx.x < kDigits)
-        for (uint32_t t = 0; t < p.tiles; ++t) {
-            const uint32_t c = p.counts[(size_t)t * kDigits + threadIdx.x];
-            mine += t < blockIdx.x ? c : 0;
-            total += c;
+        for (uint32_t t = 0; t < p.tiles; t += 8) {   // (eight loads on their way)
+            uint32_t c[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) c[u] = p.counts[(size_t)(t + u < p.tiles ? t + u : p.tiles - 1) * kDigits + threadIdx.x];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                mine += t + u < blockIdx.x ? c[u] : 0;
+                total += t + u < p.tiles ? c[u] : 0;
+            }
         }
     const uint32_t before = scan_digits(total, totals);
     if (threadIdx.x < kDigits) next[threadIdx.x] = before + mine;
@@ -211,6 +242,7 @@ __global__ __launch_bounds__(kSortThreads) void move_places_kernel(Pass p, Fill 
 #pragma unroll
         for (int u = 0; u < kTileRounds; ++u)
             if (key[u] != ~0u) {
+                if (p.flags && !p.keys) p.flags[key[u]] = 1;
                 const uint32_t to = counts[w][key[u] >> p.shift & mask] + rank[u];
                 p.keys_out[to] = key[u];
                 p.places_out[to] = place[u];
@@ -219,7 +251,7 @@ __global__ __launch_bounds__(kSortThreads) void move_places_kernel(Pass p, Fill 
     }
 }
 
-// Groups of L lanes add up runs of `run` sorted places, V columns a lane; blockIdx.y: the block of L * V columns.  A word whose places all lie in the run is written to the table; the
+// Groups of L lanes add up runs of `run` sorted places, kColumns columns a lane.  A word whose places all lie in the run is written to the table; the
 // piece of a word that began in an earlier run goes to pieces[run][0], that of one that begins here and goes on to pieces[run][1].
 struct Sum {
     const uint32_t *keys, *places;
@@ -228,45 +260,50 @@ struct Sum {
     uint32_t n, vocab, run;
     int width, accumulate;
     float scale;
+    uint32_t column_blocks, blocks;   // of L * V columns; workgroups of the sums: further ones fill
 };
-// A lane's columns: V of them from `at` on; the last ones of a row whose length is no multiple of V overlap the lane's before, by `skip` columns (V: another lane has them all).  Rows
-// shorter than V: one lane has them, value by value.
-template <int V> struct Columns {
-    int at, skip, narrow;
+// A lane's columns: V of them from `at` on; the last ones of a row whose length is no multiple of V overlap the lane's before, by `skip` columns (V: another lane has them all).  NARROW:
+// rows shorter than V, one lane's, value by value (decided when compiled: a branch around every load would wait for it).
+template <int V, bool NARROW> struct Columns {
+    int at, skip;
     __device__ __forceinline__ Columns(int chunk, int width) {
         const int last = width - V;
-        narrow = last < 0 ? width : 0;
-        at = narrow ? 0 : chunk * V > last ? last : chunk * V;
-        skip = narrow ? (chunk ? V : 0) : chunk * V >= width ? V : chunk * V - at;
+        if constexpr (NARROW) {
+            at = 0;
+            skip = chunk ? V : -last;   // (columns that there are not)
+        } else {
+            at = chunk * V > last ? last : chunk * V;
+            skip = chunk * V >= width ? V : chunk * V - at;
+        }
     }
     template <typename T> __device__ __forceinline__ Chunk<T, V> load(const T* row) const {
         Chunk<T, V> c;
-        if (!narrow) {
+        if constexpr (!NARROW) {
             c.load(row + at);
         } else {
             float v[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = i < narrow ? load_value(row + i) : 0.f;
+            for (int i = 0; i < V; ++i) v[i] = i < V - skip ? load_value(row + i) : 0.f;
             c.put(v);
         }
         return c;
     }
     template <typename T> __device__ __forceinline__ void store(T* row, const float (&v)[V]) const {
         if (skip == V) return;
-        if (!narrow) {
+        if constexpr (!NARROW) {
             Chunk<T, V> c;
             c.put(v);
             c.store(row + at);
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (i < narrow) store_value(row + i, v[i]);
+                if (i < V - skip) store_value(row + i, v[i]);
         }
     }
     // row += v: a column that two lanes hold is one's alone
     __device__ __forceinline__ void add(float* row, float (&v)[V]) const {
         if (skip == V) return;
-        if (!skip && !narrow) {
+        if (!NARROW && !skip) {
             Chunk<float, V> c;
             c.load(row + at);
 #pragma unroll
@@ -276,62 +313,77 @@ template <int V> struct Columns {
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (i >= skip && (!narrow || i < narrow)) row[at + i] += v[i];
+                if (NARROW ? i < V - skip : i >= skip) row[at + i] += v[i];
         }
     }
 };
-template <int V> __device__ __forceinline__ void put_row(const Sum& q, const Columns<V>& c, uint32_t word, float (&s)[V]) {
-    float* row = q.table + (size_t)word * q.width;
+// a word's sum to its row of the table, or, a piece of it, to `piece` (short code: it stands behind every place of a run)
+template <bool ACCUMULATE, int V, bool NARROW> __device__ __forceinline__ void put_row(const Sum& q, const Columns<V, NARROW>& c, uint32_t word, float* piece, float (&s)[V]) {
+    float* row = piece ? piece : q.table + (size_t)word * q.width;
+    const float scale = piece ? 1.f : q.scale;
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i] *= q.scale;
-    if (q.accumulate) c.add(row, s);
+    for (int i = 0; i < V; ++i) s[i] *= scale;
+    if (ACCUMULATE && !piece) c.add(row, s);
     else c.store(row, s);
 }
 
-template <typename O, int L>
-__global__ __launch_bounds__(kThreads) void sum_runs_kernel(Sum q) {
-    constexpr int V = 16 / sizeof(O), kAhead = 8;
-    const uint32_t r = blockIdx.x * (kThreads / L) + threadIdx.x / L;
+template <typename O, int L, bool NARROW, bool ACCUMULATE>
+__global__ __launch_bounds__(kThreads) void sum_runs_kernel(Sum q, Fill fill) {
+    constexpr int V = kColumns, kGroups = kThreads / L, kAhead = 8;
+    if (blockIdx.x >= q.blocks) return fill_zeros<kThreads>(fill, blockIdx.x - q.blocks, gridDim.x - q.blocks);
+    __shared__ uint32_t keys[kGroups][kMaxRun], places[kGroups][kMaxRun];   // of each group's run
+    const int l = threadIdx.x % L, group = threadIdx.x / L;
+    const uint32_t id = blockIdx.x * kGroups + group, r = id / q.column_blocks;   // (neighbours take a run's other columns: whole rows are read and written at about the same time)
     const uint64_t begin = (uint64_t)r * q.run;
     if (begin >= q.n) return;
-    const uint32_t b = (uint32_t)begin, e = q.n - b < q.run ? q.n : b + q.run;
-    const Columns<V> col(blockIdx.y * L + threadIdx.x % L, q.width);
+    const uint32_t b = (uint32_t)begin, len = q.n - b < q.run ? q.n - b : q.run;
+    for (uint32_t i = l; i < q.run; i += L) {
+        const uint32_t at = b + (i < len ? i : len - 1);
+        keys[group][i] = q.keys[at];
+        places[group][i] = q.places[at];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a group lies in one wave)
+    const uint32_t before = b ? q.keys[b - 1] : ~0u, after = b + len < q.n ? q.keys[b + len] : ~0u;
+    const Columns<V, NARROW> col((id - r * q.column_blocks) * L + l, q.width);
     float* pieces = q.pieces + (size_t)r * 2 * q.width;
-    const uint32_t before = b ? q.keys[b - 1] : ~0u;
-    uint32_t word = q.keys[b];
+    uint32_t word = keys[group][0];
     float s[V] = {};
-    for (uint32_t p = b; p < e && word < q.vocab; p += kAhead) {
-        uint32_t key[kAhead];
-        Chunk<O, V> row[kAhead];
+    Chunk<O, V> rows[2][kAhead];   // one set on its way while the other is added up
+    auto fetch = [&](Chunk<O, V>(&row)[kAhead], uint32_t p) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) row[u] = col.load((const O*)q.dout + (size_t)places[group][p + u] * q.width);
+    };
+    auto add = [&](const Chunk<O, V>(&row)[kAhead], uint32_t p) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const uint32_t at = p + u < e ? p + u : e - 1;
-            key[u] = q.keys[at];
-            row[u] = col.load((const O*)q.dout + (size_t)q.places[at] * q.width);
-        }
+            const uint32_t key = keys[group][p + u];
+            if (p + u < len) {
+                if (key != word) {
+                    put_row<ACCUMULATE>(q, col, word, word == before ? pieces : nullptr, s);   // (a word before another one is in the vocabulary)
+                    word = key;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (p + u >= e) break;
-            if (key[u] != word) {
-                if (word == before) col.store(pieces, s);
-                else put_row(q, col, word, s);
-                word = key[u];
+                    for (int i = 0; i < V; ++i) s[i] = 0.f;
+                }
 #pragma unroll
-                for (int i = 0; i < V; ++i) s[i] = 0.f;
-                if (word == q.vocab) break;
+                for (int i = 0; i < V; ++i) s[i] += row[u].get(i);
             }
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[i] += row[u].get(i);
         }
+    };
+    fetch(rows[0], 0);
+    for (uint32_t p = 0; p < len; p += 2 * kAhead) {
+        if (p + kAhead < len) fetch(rows[1], p + kAhead);
+        add(rows[0], p);
+        if (p + kAhead >= len) break;
+        if (p + 2 * kAhead < len) fetch(rows[0], p + 2 * kAhead);
+        add(rows[1], p + kAhead);
     }
     if (word == q.vocab) return;
-    if (word == before) col.store(pieces, s);
-    else if (e < q.n && q.keys[e] == word) col.store(pieces + q.width, s);
-    else put_row(q, col, word, s);
+    put_row<ACCUMULATE>(q, col, word, word == before ? pieces : word == after ? pieces + q.width : nullptr, s);
 }
 
 // A workgroup per run (and 256 columns): where a word begins in the run and goes on beyond it, its pieces are added up, every kJoinWaves-th by a wave, and its row is written.
 constexpr int kJoinWaves = 4;
+template <bool NARROW>
 __global__ __launch_bounds__(kJoinWaves * kWave) void join_pieces_kernel(Sum q, uint32_t runs) {
     constexpr int V = 4, kAhead = 4;
     __shared__ float lds[kJoinWaves][kWave][V];
@@ -350,7 +402,7 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void join_pieces_kernel(Sum q, 
         }
         more += kWave;
     }
-    const Columns<V> col(blockIdx.y * kWave + lane, q.width);
+    const Columns<V, NARROW> col(blockIdx.y * kWave + lane, q.width);
     const size_t step = 2 * (size_t)q.width;
     const float* from = q.pieces + (size_t)r * step;
     float s[V] = {};
@@ -379,7 +431,8 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void join_pieces_kernel(Sum q, 
     for (int v = 1; v < kJoinWaves; ++v)
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] += lds[v][lane][i];
-    put_row(q, col, word, s);
+    if (q.accumulate) put_row<true>(q, col, word, nullptr, s);
+    else put_row<false>(q, col, word, nullptr, s);
 }
 
 int check_desc(const flashrnn_embedding_desc_t* d, bool gradient) {
@@ -395,9 +448,9 @@ int check_desc(const flashrnn_embedding_desc_t* d, bool gradient) {
 struct Plan {
     int passes, bits;
     uint32_t tiles, span;   // tiles = 0: the sort of one workgroup
-    int L, blocks_y;
+    int L, column_blocks;
     uint32_t run, runs;
-    size_t keys[2], places[2], counts, pieces, total;
+    size_t keys[2], places[2], counts, flags, pieces, total;
 };
 Plan plan_of(const flashrnn_embedding_desc_t* d) {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
@@ -414,13 +467,13 @@ Plan plan_of(const flashrnn_embedding_desc_t* d) {
         p.tiles = (uint32_t)((n + p.span - 1) / p.span);
     }
     // lanes per row: the number that leaves the fewest of them without columns, the larger one of equals
-    const int V = 16 / (int)type_size(d->io_dtype), chunks = (d->width + V - 1) / V;
+    const int chunks = (d->width + kColumns - 1) / kColumns;
     p.L = 64;
     for (int L = 32; L >= 8; L /= 2)
         if ((chunks + L - 1) / L * L < (chunks + p.L - 1) / p.L * p.L) p.L = L;
-    p.blocks_y = (chunks + p.L - 1) / p.L;
+    p.column_blocks = (chunks + p.L - 1) / p.L;
     // places per run: enough runs for 2048 waves, as long as that leaves them kMinRun places or more
-    const size_t waves = n * p.blocks_y * p.L / kWave;
+    const size_t waves = n * p.column_blocks * p.L / kWave;
     p.run = kMaxRun;
     while (p.run > kMinRun && waves / p.run < 2048) p.run /= 2;
     p.runs = (uint32_t)((n + p.run - 1) / p.run);
@@ -431,6 +484,7 @@ Plan plan_of(const flashrnn_embedding_desc_t* d) {
         p.places[i] = at; at += list;
     }
     p.counts = at; at += up((size_t)p.tiles * kDigits * 4);
+    p.flags = at; at += p.tiles ? up((size_t)d->vocab + 1) : 0;
     p.pieces = at; at += up((size_t)p.runs * 2 * d->width * 4);
     p.total = at + 256;
     return p;
@@ -472,49 +526,65 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
     const hipStream_t stream = (hipStream_t)hip_stream;
     const Plan p = plan_of(d);
     char* ws = (char*)workspace;
-    const size_t floats = accumulate ? 0 : (size_t)d->vocab * d->width;
-    const size_t per_block = kSortThreads * 4 * 4;   // floats that a workgroup fills at least
-    auto fill_blocks = [&](const Fill& f) { return (unsigned)((f.end - f.begin + per_block - 1) / per_block < kFillBlocks ? (f.end - f.begin + per_block - 1) / per_block : kFillBlocks); };
+    const size_t row_bytes = (size_t)d->width * 4;
+    Fill fill{(float*)dtable, nullptr, 0, 0, (uint32_t)(row_bytes >= kFillBytes ? 1 : row_bytes * kWave <= kFillBytes ? kWave : kFillBytes / row_bytes), d->width};
+    auto fill_to = [&](uint32_t end, int waves) {   // the rows behind those filled so far; the workgroups for them
+        fill.begin = fill.end;
+        fill.end = accumulate ? 0 : end;
+        const size_t parts = ((size_t)fill.end - fill.begin + fill.each - 1) / fill.each, blocks = (parts + waves - 1) / waves;
+        return (unsigned)(blocks < kFillBlocks ? blocks : kFillBlocks);
+    };
+    const uint32_t vocab = (uint32_t)d->vocab;
     uint32_t *keys = (uint32_t*)(ws + p.keys[0]), *places = (uint32_t*)(ws + p.places[0]);
     if (p.tiles == 0) {
-        const Fill fill{(float*)dtable, 0, floats};
-        hipLaunchKernelGGL(sort_small_kernel, dim3(1 + fill_blocks(fill)), dim3(kSortThreads), 0, stream, tokens, d->index_dtype == FLASHRNN_I64, (uint32_t)n, (uint32_t)d->vocab,
-                           p.passes, p.bits, keys, places, fill);
+        const unsigned blocks = fill_to(vocab, kSortWaves);
+        hipLaunchKernelGGL(sort_small_kernel, dim3(1 + blocks), dim3(kSortThreads), 0, stream, tokens, d->index_dtype == FLASHRNN_I64, (uint32_t)n, vocab, p.passes, p.bits, keys, places,
+                           fill);
         if (const int e = launch_status()) return e;
         if (n == 0) return FLASHRNN_OK;
     } else {
-        const size_t share = (floats / (2 * p.passes) + 3) / 4 * 4;   // of the table, that one launch of the sort fills
-        size_t filled = 0;
-        Pass q{tokens, nullptr, nullptr, nullptr, nullptr, (uint32_t*)(ws + p.counts), (uint32_t)n, p.span, p.tiles, (uint32_t)d->vocab, 0, p.bits, d->index_dtype == FLASHRNN_I64};
+        uint8_t* flags = accumulate ? nullptr : (uint8_t*)(ws + p.flags);
+        const size_t rows_at_a_time = kFillBesideSort / row_bytes;
+        Pass q{tokens, nullptr, nullptr, nullptr, nullptr, (uint32_t*)(ws + p.counts), flags, (uint32_t)n, p.span, p.tiles, vocab, 0, p.bits, d->index_dtype == FLASHRNN_I64};
         for (int pass = 0; pass < p.passes; ++pass) {
             q.shift = pass * p.bits;
             q.keys_out = keys = (uint32_t*)(ws + p.keys[pass & 1]);
             q.places_out = places = (uint32_t*)(ws + p.places[pass & 1]);
             for (int step = 0; step < 2; ++step) {
-                const bool last = step == 1 && pass == p.passes - 1;
-                const Fill fill{(float*)dtable, filled, last || filled + share > floats ? floats : filled + share};
-                filled = fill.end;
-                const dim3 grid(p.tiles + fill_blocks(fill));
+                unsigned more = 0;   // workgroups beside the sort
+                if (pass) more = fill_to(rows_at_a_time < vocab - fill.end ? fill.end + (uint32_t)rows_at_a_time : vocab, kSortWaves);
+                else if (step == 0 && flags) more = vocab / kFlagsPerBlock < kFillBlocks ? 1 + vocab / kFlagsPerBlock : kFillBlocks;
+                const dim3 grid(p.tiles + more);
                 if (step == 0) hipLaunchKernelGGL(count_digits_kernel, grid, dim3(kSortThreads), 0, stream, q, fill);
                 else hipLaunchKernelGGL(move_places_kernel, grid, dim3(kSortThreads), 0, stream, q, fill);
                 if (const int e = launch_status()) return e;
+                fill.flags = flags;
             }
             q.keys = keys;
             q.places = places;
         }
     }
-    const Sum q{keys, places, dout, (float*)dtable, (float*)(ws + p.pieces), (uint32_t)n, (uint32_t)d->vocab, p.run, d->width, accumulate, d->scale};
+    const unsigned fill_blocks = fill_to(vocab, kThreads / kWave);   // (with few places: none are left)
+    const uint32_t sum_blocks = (uint32_t)(((size_t)p.runs * p.column_blocks + kThreads / p.L - 1) / (kThreads / p.L));
+    const Sum q{keys, places, dout, (float*)dtable, (float*)(ws + p.pieces), (uint32_t)n, vocab, p.run, d->width, accumulate, d->scale, (uint32_t)p.column_blocks, sum_blocks};
     const int e = with_io_type(d->io_dtype, [&](auto* ot) {
         using O = std::remove_pointer_t<decltype(ot)>;
-        const dim3 grid((p.runs + kThreads / p.L - 1) / (kThreads / p.L), p.blocks_y);
-        if (p.L == 64) hipLaunchKernelGGL((sum_runs_kernel<O, 64>), grid, dim3(kThreads), 0, stream, q);
-        else if (p.L == 32) hipLaunchKernelGGL((sum_runs_kernel<O, 32>), grid, dim3(kThreads), 0, stream, q);
-        else if (p.L == 16) hipLaunchKernelGGL((sum_runs_kernel<O, 16>), grid, dim3(kThreads), 0, stream, q);
-        else hipLaunchKernelGGL((sum_runs_kernel<O, 8>), grid, dim3(kThreads), 0, stream, q);
+        const dim3 grid(sum_blocks + fill_blocks);
+        auto launch = [&](auto lanes, auto narrow) {
+            if (accumulate) hipLaunchKernelGGL((sum_runs_kernel<O, decltype(lanes)::value, decltype(narrow)::value, true>), grid, dim3(kThreads), 0, stream, q, fill);
+            else hipLaunchKernelGGL((sum_runs_kernel<O, decltype(lanes)::value, decltype(narrow)::value, false>), grid, dim3(kThreads), 0, stream, q, fill);
+        };
+        if (d->width < kColumns) launch(Int<8>{}, Int<1>{});
+        else if (p.L == 64) launch(Int<64>{}, Int<0>{});
+        else if (p.L == 32) launch(Int<32>{}, Int<0>{});
+        else if (p.L == 16) launch(Int<16>{}, Int<0>{});
+        else launch(Int<8>{}, Int<0>{});
         return launch_status();
     });
     if (e != FLASHRNN_OK || p.runs == 1) return e;
-    hipLaunchKernelGGL(join_pieces_kernel, dim3(p.runs, (d->width + 4 * kWave - 1) / (4 * kWave)), dim3(kJoinWaves * kWave), 0, stream, q, p.runs);
+    const dim3 grid(p.runs, (d->width + 4 * kWave - 1) / (4 * kWave));
+    if (d->width < 4) hipLaunchKernelGGL((join_pieces_kernel<true>), grid, dim3(kJoinWaves * kWave), 0, stream, q, p.runs);
+    else hipLaunchKernelGGL((join_pieces_kernel<false>), grid, dim3(kJoinWaves * kWave), 0, stream, q, p.runs);
     return launch_status();
 }
 

@@ -376,7 +376,6 @@ int strips_of(const flashrnn_layer_norm_desc_t* d) {
     return tokens < kMaxStrips ? (tokens ? (int)tokens : 1) : kMaxStrips;
 }
 
-template <int N> struct Int { static constexpr int value = N; };
 // calls f(X*, Y*, V, shape) for a gradient whose rows fit in registers
 template <typename F> void with_grad_shape(const flashrnn_layer_norm_desc_t* d, F&& f) {
     if (d->width < 8) return;

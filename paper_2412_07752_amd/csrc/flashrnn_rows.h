@@ -214,6 +214,7 @@ template <int K = 3, typename F> bool with_long_shape(int chunks, F&& f) {
     }
 }
 
+template <int N> struct Int { static constexpr int value = N; };
 // calls f with a null pointer of the C++ type behind a flashrnn_dtype_t / flashrnn_index_t
 template <typename F> int with_io_type(int t, F&& f) { return t == FLASHRNN_BF16 ? f((__bf16*)nullptr) : f((float*)nullptr); }
 template <typename F> int with_index_type(int t, F&& f) { return t == FLASHRNN_I64 ? f((int64_t*)nullptr) : f((int32_t*)nullptr); }
