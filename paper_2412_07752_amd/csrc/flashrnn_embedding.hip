@@ -18,6 +18,8 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / kWave;
 constexpr int kRounds = kSmall / kSortThreads;   // places per thread of the one workgroup
 constexpr int kTileRounds = 2;                   // ... of a tile at a time
+constexpr int kRows = 4;           // places that a group of lanes looks up at a time, where there are kManyWaves waves of places
+constexpr uint64_t kManyWaves = 16384;
 constexpr int kColumns = 4;        // columns a lane adds up: neighbours store whole cache lines of float32 (with eight, each store left every second 16 bytes out)
 constexpr uint32_t kMinRun = 8, kMaxRun = 64;   // sorted places that a group of lanes adds up
 constexpr size_t kFillBlocks = 2048, kFillBytes = 8 << 10;   // workgroups that fill, at most; bytes of the table that a wave fills at a time
@@ -29,12 +31,91 @@ __device__ __forceinline__ uint32_t key_of(const void* tokens, bool index64, siz
     return t >= 0 && t < (int64_t)vocab ? (uint32_t)t : vocab;
 }
 
-template <typename E, typename O, typename I>
-__global__ __launch_bounds__(kThreads) void embedding_fwd_kernel(size_t n, int vocab, int width, const E* __restrict__ table, const I* __restrict__ tokens, O* __restrict__ out, float scale) {
-    for (size_t row = blockIdx.x; row < n; row += gridDim.x) {
-        const int64_t t = tokens[row];
-        const bool there = t >= 0 && t < vocab;
-        for (int j = threadIdx.x; j < width; j += kThreads) store_value(out + row * width + j, there ? load_value(table + (size_t)t * width + j) * scale : 0.f);
+// A lane's columns: V of them from `at` on; the last ones of a row whose length is no multiple of V overlap the lane's before, by `skip` columns (V: another lane has them all).  NARROW:
+// rows shorter than V, one lane's, value by value (decided when compiled: a branch around every load would wait for it).
+template <int V, bool NARROW> struct Columns {
+    int at, skip;
+    __device__ __forceinline__ Columns(int chunk, int width) {
+        const int last = width - V;
+        if constexpr (NARROW) {
+            at = 0;
+            skip = chunk ? V : -last;   // (columns that there are not)
+        } else {
+            at = chunk * V > last ? last : chunk * V;
+            skip = chunk * V >= width ? V : chunk * V - at;
+        }
+    }
+    template <typename T> __device__ __forceinline__ Chunk<T, V> load(const T* row) const {
+        Chunk<T, V> c;
+        if constexpr (!NARROW) {
+            c.load(row + at);
+        } else {
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = i < V - skip ? load_value(row + i) : 0.f;
+            c.put(v);
+        }
+        return c;
+    }
+    template <typename T> __device__ __forceinline__ void store(T* row, const float (&v)[V], bool stream = false) const {
+        if (skip == V) return;
+        if constexpr (!NARROW) {
+            Chunk<T, V> c;
+            c.put(v);
+            c.store(row + at, stream);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < V - skip) store_value(row + i, v[i]);
+        }
+    }
+    // row += v: a column that two lanes hold is one's alone
+    __device__ __forceinline__ void add(float* row, float (&v)[V]) const {
+        if (skip == V) return;
+        if (!NARROW && !skip) {
+            Chunk<float, V> c;
+            c.load(row + at);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += c.get(i);
+            c.put(v);
+            c.store(row + at);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (NARROW ? i < V - skip : i >= skip) row[at + i] += v[i];
+        }
+    }
+};
+
+// Lookup: groups of L lanes take V columns a lane of `rows` places each, whose words and then whose rows are requested together.
+struct Lookup {
+    const void *table, *tokens;
+    void* out;
+    uint64_t n;
+    uint32_t vocab, column_blocks;
+    int width, index64, stream;
+    float scale;
+};
+template <typename E, typename O, int L, int R, bool NARROW>
+__global__ __launch_bounds__(kThreads) void embedding_fwd_kernel(Lookup q) {
+    constexpr int V = sizeof(E) == 2 && sizeof(O) == 2 ? 8 : 4, kGroups = kThreads / L;
+    const uint64_t step = (uint64_t)gridDim.x * kGroups, total = (q.n + R - 1) / R * q.column_blocks;
+    for (uint64_t id = (uint64_t)blockIdx.x * kGroups + threadIdx.x / L; id < total; id += step) {
+        const uint64_t part = id / q.column_blocks, first = part * R;
+        const Columns<V, NARROW> col((int)(id - part * q.column_blocks) * L + threadIdx.x % L, q.width);
+        uint32_t word[R];
+#pragma unroll
+        for (int u = 0; u < R; ++u) word[u] = key_of(q.tokens, q.index64, first + u < q.n ? first + u : q.n - 1, q.vocab);
+        Chunk<E, V> row[R];
+#pragma unroll
+        for (int u = 0; u < R; ++u) row[u] = col.load((const E*)q.table + (size_t)(word[u] < q.vocab ? word[u] : 0) * q.width);   // (row 0 for places outside the vocabulary)
+#pragma unroll
+        for (int u = 0; u < R; ++u) {
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = word[u] < q.vocab ? row[u].get(i) * q.scale : 0.f;
+            if (first + u < q.n) col.store((O*)q.out + (size_t)(first + u) * q.width, v, q.stream);
+        }
     }
 }
 
@@ -262,61 +343,6 @@ struct Sum {
     float scale;
     uint32_t column_blocks, blocks;   // of L * V columns; workgroups of the sums: further ones fill
 };
-// A lane's columns: V of them from `at` on; the last ones of a row whose length is no multiple of V overlap the lane's before, by `skip` columns (V: another lane has them all).  NARROW:
-// rows shorter than V, one lane's, value by value (decided when compiled: a branch around every load would wait for it).
-template <int V, bool NARROW> struct Columns {
-    int at, skip;
-    __device__ __forceinline__ Columns(int chunk, int width) {
-        const int last = width - V;
-        if constexpr (NARROW) {
-            at = 0;
-            skip = chunk ? V : -last;   // (columns that there are not)
-        } else {
-            at = chunk * V > last ? last : chunk * V;
-            skip = chunk * V >= width ? V : chunk * V - at;
-        }
-    }
-    template <typename T> __device__ __forceinline__ Chunk<T, V> load(const T* row) const {
-        Chunk<T, V> c;
-        if constexpr (!NARROW) {
-            c.load(row + at);
-        } else {
-            float v[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = i < V - skip ? load_value(row + i) : 0.f;
-            c.put(v);
-        }
-        return c;
-    }
-    template <typename T> __device__ __forceinline__ void store(T* row, const float (&v)[V]) const {
-        if (skip == V) return;
-        if constexpr (!NARROW) {
-            Chunk<T, V> c;
-            c.put(v);
-            c.store(row + at);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (i < V - skip) store_value(row + i, v[i]);
-        }
-    }
-    // row += v: a column that two lanes hold is one's alone
-    __device__ __forceinline__ void add(float* row, float (&v)[V]) const {
-        if (skip == V) return;
-        if (!NARROW && !skip) {
-            Chunk<float, V> c;
-            c.load(row + at);
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] += c.get(i);
-            c.put(v);
-            c.store(row + at);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (NARROW ? i < V - skip : i >= skip) row[at + i] += v[i];
-        }
-    }
-};
 // a word's sum to its row of the table, or, a piece of it, to `piece` (short code: it stands behind every place of a run)
 template <bool ACCUMULATE, int V, bool NARROW> __device__ __forceinline__ void put_row(const Sum& q, const Columns<V, NARROW>& c, uint32_t word, float* piece, float (&s)[V]) {
     float* row = piece ? piece : q.table + (size_t)word * q.width;
@@ -444,6 +470,14 @@ int check_desc(const flashrnn_embedding_desc_t* d, bool gradient) {
     return FLASHRNN_OK;
 }
 
+// lanes per row: the number that leaves the fewest of them without columns, the larger one of equals
+int lanes_for(int chunks) {
+    int best = 64;
+    for (int L = 32; L >= 8; L /= 2)
+        if ((chunks + L - 1) / L * L < (chunks + best - 1) / best * best) best = L;
+    return best;
+}
+
 // How the gradient is laid out: the sort's passes and tiles, the runs, the workspace.
 struct Plan {
     int passes, bits;
@@ -466,11 +500,8 @@ Plan plan_of(const flashrnn_embedding_desc_t* d) {
         p.span = (uint32_t)(each * step);
         p.tiles = (uint32_t)((n + p.span - 1) / p.span);
     }
-    // lanes per row: the number that leaves the fewest of them without columns, the larger one of equals
     const int chunks = (d->width + kColumns - 1) / kColumns;
-    p.L = 64;
-    for (int L = 32; L >= 8; L /= 2)
-        if ((chunks + L - 1) / L * L < (chunks + p.L - 1) / p.L * p.L) p.L = L;
+    p.L = lanes_for(chunks);
     p.column_blocks = (chunks + p.L - 1) / p.L;
     // places per run: enough runs for 2048 waves, as long as that leaves them kMinRun places or more
     const size_t waves = n * p.column_blocks * p.L / kWave;
@@ -504,14 +535,28 @@ int flashrnn_embedding_fwd(const flashrnn_embedding_desc_t* d, const void* table
     if (!aligned_to(table, type_size(d->table_dtype)) || !aligned_to(out, type_size(d->io_dtype)) || !aligned_to(tokens, type_size(d->index_dtype))) return FLASHRNN_ERR_UNSUPPORTED;
     return with_io_type(d->table_dtype, [&](auto* et) {
         return with_io_type(d->io_dtype, [&](auto* ot) {
-            return with_index_type(d->index_dtype, [&](auto* it) {
-                using E = std::remove_pointer_t<decltype(et)>;
-                using O = std::remove_pointer_t<decltype(ot)>;
-                using I = std::remove_pointer_t<decltype(it)>;
-                hipLaunchKernelGGL((embedding_fwd_kernel<E, O, I>), dim3(row_blocks((size_t)d->tokens)), dim3(kThreads), 0, (hipStream_t)hip_stream, (size_t)d->tokens, d->vocab, d->width, (const E*)table,
-                                   (const I*)tokens, (O*)out, d->scale);
-                return launch_status();
-            });
+            using E = std::remove_pointer_t<decltype(et)>;
+            using O = std::remove_pointer_t<decltype(ot)>;
+            constexpr int V = sizeof(E) == 2 && sizeof(O) == 2 ? 8 : 4;
+            const int chunks = (d->width + V - 1) / V, L = lanes_for(chunks);
+            const uint64_t n = (uint64_t)d->tokens;
+            const uint32_t column_blocks = (uint32_t)((chunks + L - 1) / L);
+            const Lookup q{table, tokens, out, n, (uint32_t)d->vocab, column_blocks, d->width, d->index_dtype == FLASHRNN_I64, n * d->width * sizeof(O) > kStreamBytes, d->scale};
+            const bool many = n * column_blocks * L / kWave >= kManyWaves;
+            auto launch = [&](auto lanes, auto narrow) {
+                constexpr int kLanes = decltype(lanes)::value;
+                constexpr bool kNarrow = decltype(narrow)::value;
+                const uint64_t groups = (n + (many ? kRows : 1) - 1) / (many ? kRows : 1) * column_blocks;
+                const dim3 grid(row_blocks((groups + kThreads / kLanes - 1) / (kThreads / kLanes)));
+                if (many) hipLaunchKernelGGL((embedding_fwd_kernel<E, O, kLanes, kRows, kNarrow>), grid, dim3(kThreads), 0, (hipStream_t)hip_stream, q);
+                else hipLaunchKernelGGL((embedding_fwd_kernel<E, O, kLanes, 1, kNarrow>), grid, dim3(kThreads), 0, (hipStream_t)hip_stream, q);
+            };
+            if (d->width < V) launch(Int<8>{}, Int<1>{});
+            else if (L == 64) launch(Int<64>{}, Int<0>{});
+            else if (L == 32) launch(Int<32>{}, Int<0>{});
+            else if (L == 16) launch(Int<16>{}, Int<0>{});
+            else launch(Int<8>{}, Int<0>{});
+            return launch_status();
         });
     });
 }
