@@ -310,7 +310,7 @@ int flashrnn_cross_entropy(const flashrnn_cross_entropy_desc_t* desc, const void
  * Clipping by the global norm:  norm = sqrt(sum of the squares of all values of all tensors),  factor = 1 where norm <= max_norm, else
  * max_norm / norm,  out_k = factor * grad_k.  The squares are added in 64 bits, in a fixed order.  A NaN or an infinity in any tensor makes the norm NaN or infinite
  * and goes through the same formula (NaN: every value becomes NaN).
- *   count       number of tensors
+ *   count       number of tensors, at most 2^24
  *   grads, out  HOST arrays of `count` device pointers; out[k] may be grads[k] (in place: nothing is written where the factor is 1), and out may be
  *               NULL (the norm alone); any other overlap is undefined
  *   sizes       HOST array: values per tensor, >= 0

@@ -7,6 +7,7 @@ namespace {
 
 constexpr int kTensors = 128;      // tensors per launch: their table is a kernel argument, which holds 4 KB
 constexpr int kMaxBlocks = 2048;   // workgroups per launch, each with a partial sum
+constexpr int kMaxCount = 1 << 24;
 constexpr int kChunk = 8192;       // values of one tensor that a workgroup takes at a time
 
 struct Table {
@@ -27,46 +28,91 @@ __device__ __forceinline__ int tensor_of(const Table& t, int chunk) {
     return lo;
 }
 
+// f(in, out, values) for chunks blockIdx.x, blockIdx.x + gridDim.x, ...  (Going through them backwards in the second kernel, so that it begins with what was read last, changes nothing: 742 us and
+// 738 for 330 M values, 176 and 177 for 73 M.)
 template <typename F> __device__ __forceinline__ void for_chunks(const Table& t, F&& f) {
     for (int chunk = blockIdx.x; chunk < t.first_chunk[t.count]; chunk += gridDim.x) {
         const int k = tensor_of(t, chunk);
-        const size_t n = (size_t)(t.size[k] < 0 ? ~t.size[k] : t.size[k]), begin = (size_t)(chunk - t.first_chunk[k]) * kChunk;
-        const size_t end = begin + kChunk < n ? begin + kChunk : n;
-        if (t.size[k] < 0) f((const __bf16*)t.in[k], (__bf16*)t.out[k], begin, end);
-        else f((const float*)t.in[k], (float*)t.out[k], begin, end);
+        const long long n = t.size[k] < 0 ? ~t.size[k] : t.size[k], begin = (long long)(chunk - t.first_chunk[k]) * kChunk;
+        const int count = n - begin < kChunk ? (int)(n - begin) : kChunk;
+        if (t.size[k] < 0) f((const __bf16*)t.in[k] + begin, (__bf16*)t.out[k] + begin, count);
+        else f((const float*)t.in[k] + begin, (float*)t.out[k] + begin, count);
     }
 }
 
+// The sum of the squares, in 64 bits: a float32 square may leave float32's range, and its sum over a model's gradients loses the small tensors.
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(Table t, double* __restrict__ part) {
     __shared__ double lds[kThreads / kWave];
     double s = 0.0;
-    for_chunks(t, [&](auto* in, auto*, size_t begin, size_t end) {
-        for (size_t j = begin + threadIdx.x; j < end; j += kThreads) {
-            const double v = load_value(in + j);
-            s += v * v;
+    auto add = [&](float x) {
+        const double v = x;
+        s = fma(v, v, s);
+    };
+    for_chunks(t, [&](auto* in, auto*, int count) {
+        using T = std::remove_const_t<std::remove_pointer_t<decltype(in)>>;
+        constexpr int V = 16 / sizeof(T), kRounds = kChunk / (kThreads * V);
+        if (count == kChunk) {
+            Chunk<T, V> c[kRounds];
+#pragma unroll
+            for (int u = 0; u < kRounds; ++u) c[u].load(in + (u * kThreads + threadIdx.x) * V);
+#pragma unroll
+            for (int u = 0; u < kRounds; ++u)
+#pragma unroll
+                for (int i = 0; i < V; ++i) add(c[u].get(i));
+        } else {
+            for (int at = threadIdx.x * V; at < count; at += kThreads * V) {
+                if (at + V <= count) {
+                    Chunk<T, V> c;
+                    c.load(in + at);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) add(c.get(i));
+                } else {
+                    for (int i = at; i < count; ++i) add(load_value(in + i));
+                }
+            }
         }
     });
     s = block_sum<kThreads>(s, lds);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-// the norm, and the factor behind the partial sums
-__global__ __launch_bounds__(kThreads) void grad_factor_kernel(double* __restrict__ part, int count, float max_norm, float* __restrict__ norm_out) {
+// The norm and the factor from all partial sums, in every workgroup the same (a launch of its own for them takes longer than reading them again), then the products.
+__global__ __launch_bounds__(kThreads) void grad_scale_kernel(Table t, const double* __restrict__ part, int parts, float max_norm, float* __restrict__ norm_out, bool stream) {
     __shared__ double lds[kThreads / kWave];
     double s = 0.0;
-    for (int i = threadIdx.x; i < count; i += kThreads) s += part[i];
+    for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
     const double norm = sqrt(block_sum<kThreads>(s, lds));
-    if (threadIdx.x == 0) {
-        norm_out[0] = (float)norm;
-        part[count] = norm <= max_norm ? 1.0 : max_norm / norm;
-    }
-}
-
-__global__ __launch_bounds__(kThreads) void grad_scale_kernel(Table t, const double* __restrict__ factor_in) {
-    const float factor = (float)*factor_in;
-    for_chunks(t, [&](auto* in, auto* out, size_t begin, size_t end) {
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+    const float factor = norm <= max_norm ? 1.f : (float)(max_norm / norm);
+    for_chunks(t, [&](auto* in, auto* out, int count) {
+        using T = std::remove_pointer_t<decltype(out)>;
+        constexpr int V = 16 / sizeof(T), kRounds = kChunk / (kThreads * V);
         if (in == out && factor == 1.f) return;
-        for (size_t j = begin + threadIdx.x; j < end; j += kThreads) store_value(out + j, load_value(in + j) * factor);
+        auto put = [&](const Chunk<T, V>& c, int at) {
+            float v[V];
+            Chunk<T, V> o;
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = c.get(i) * factor;
+            o.put(v);
+            o.store(out + at, stream);
+        };
+        if (count == kChunk) {
+            Chunk<T, V> c[kRounds];
+#pragma unroll
+            for (int u = 0; u < kRounds; ++u) c[u].load(in + (u * kThreads + threadIdx.x) * V);
+#pragma unroll
+            for (int u = 0; u < kRounds; ++u) put(c[u], (u * kThreads + threadIdx.x) * V);
+        } else {
+            for (int at = threadIdx.x * V; at < count; at += kThreads * V) {
+                if (at + V <= count) {
+                    Chunk<T, V> c;
+                    c.load(in + at);
+                    put(c, at);
+                } else {
+                    for (int i = at; i < count; ++i) store_value(out + i, load_value(in + i) * factor);
+                }
+            }
+        }
     });
 }
 
@@ -77,20 +123,23 @@ int tables_of(int count) { return count / kTensors + (count % kTensors != 0); }
 extern "C" {
 
 size_t flashrnn_grad_clip_workspace_bytes(int count) {
-    if (count < 0) return 0;
+    if (count < 0 || count > kMaxCount) return 0;
     return ((size_t)tables_of(count) * kMaxBlocks + 1) * sizeof(double) / 256 * 256 + 256;
 }
 
 int flashrnn_grad_clip(int count, const void* const* grads, void* const* out, const long long* sizes, const int* dtypes, float max_norm, void* norm, void* workspace,
                        void* hip_stream) {
     if (count < 0 || !(max_norm >= 0.f)) return FLASHRNN_ERR_SHAPE;
+    if (count > kMaxCount) return FLASHRNN_ERR_UNSUPPORTED;
     if (!norm || (count && (!grads || !sizes || !dtypes))) return FLASHRNN_ERR_NULL;
     if (!workspace || !aligned_to(workspace, 256)) return FLASHRNN_ERR_WORKSPACE;
     if (!aligned_to(norm, 4)) return FLASHRNN_ERR_UNSUPPORTED;
+    double bytes = 0;
     for (int k = 0; k < count; ++k) {
         if (sizes[k] < 0 || !is_io_type(dtypes[k])) return FLASHRNN_ERR_SHAPE;
         if (sizes[k] && (!grads[k] || (out && !out[k]))) return FLASHRNN_ERR_NULL;
         if (!aligned_to(grads[k], type_size(dtypes[k])) || (out && !aligned_to(out[k], type_size(dtypes[k])))) return FLASHRNN_ERR_UNSUPPORTED;
+        bytes += (double)sizes[k] * type_size(dtypes[k]);
         if (sizes[k] > (1LL << 40)) return FLASHRNN_ERR_UNSUPPORTED;   // (chunks of a table are counted in 32 bits)
     }
     const hipStream_t stream = (hipStream_t)hip_stream;
@@ -120,14 +169,19 @@ int flashrnn_grad_clip(int count, const void* const* grads, void* const* out, co
         if (const int e = launch_status()) return e;
         parts += blocks;
     }
-    hipLaunchKernelGGL(grad_factor_kernel, dim3(1), dim3(kThreads), 0, stream, part, parts, max_norm, (float*)norm);
-    if (const int e = launch_status()) return e;
-    if (!out) return FLASHRNN_OK;
-    for (int first = 0; first < count; first += kTensors) {
-        const int blocks = fill(first);
-        if (blocks == 0) continue;
-        hipLaunchKernelGGL(grad_scale_kernel, dim3(blocks), dim3(kThreads), 0, stream, t, (const double*)(part + parts));
+    // (a table without values, or no table: a launch that leaves the norm alone)
+    bool told = false;
+    for (int first = 0; first < count || !told; first += kTensors) {
+        const int blocks = out ? fill(first) : 0;
+        if (blocks == 0) {
+            if (told || first + kTensors < count) continue;
+            t.count = 0;
+            t.first_chunk[0] = 0;
+        }
+        hipLaunchKernelGGL(grad_scale_kernel, dim3(blocks ? blocks : 1), dim3(kThreads), 0, stream, t, (const double*)part, parts, max_norm, told ? nullptr : (float*)norm,
+                           bytes > kStreamBytes);
         if (const int e = launch_status()) return e;
+        told = true;
     }
     return FLASHRNN_OK;
 }
