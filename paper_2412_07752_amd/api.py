@@ -139,6 +139,9 @@ def lib():
         native = _load_native()
         if native is not None:
             native.bind(*(ctypes.cast(f, vp).value for f in (L.flashrnn_fwd, L.flashrnn_fwd_static_scratch, L.flashrnn_num_states, L.flashrnn_num_gates)))
+            native.bind_operators(*(ctypes.cast(f, vp).value for f in (
+                L.flashrnn_embedding_fwd, L.flashrnn_embedding_bwd, L.flashrnn_embedding_workspace_bytes, L.flashrnn_layer_norm_fwd, L.flashrnn_layer_norm_bwd,
+                L.flashrnn_layer_norm_workspace_bytes, L.flashrnn_cross_entropy, L.flashrnn_grad_clip, L.flashrnn_grad_clip_workspace_bytes)))
         _lib, _native = L, native
     return _lib
 
@@ -419,6 +422,12 @@ def _index_dtype(t):
     raise TypeError(f"tokens and targets must be int64 or int32, got {t.dtype}")
 
 
+def _done(rc, where, result):
+    if rc != FLASHRNN_OK:
+        raise FlashRNNError(rc, where)
+    return result
+
+
 def _same_device(first, **others):
     for name, t in others.items():
         if t is not None and t.device != first.device:
@@ -443,6 +452,10 @@ def flashrnn_embedding_workspace_bytes(tokens, vocab, width=1):
 def flashrnn_embedding_fwd(table, tokens, scale=1.0, dtype=None, out=None, stream=None):
     """out[..., :] = scale * table[tokens[...], :], in the table's type or in `dtype`.  table[vocab, width] bf16 or f32, tokens of any shape, int64 or int32;
     tokens outside the vocabulary give zeros."""
+    if _native is not None and stream is None and out is not None:
+        rc = _native.embedding_fwd(table, tokens, scale, out)
+        if rc <= 0:
+            return _done(rc, "flashrnn_embedding_fwd", out)
     V, H = table.shape
     dtype = (table.dtype if dtype is None else dtype) if out is None else out.dtype
     _chk(table, (V, H), table.dtype, "table")
@@ -461,6 +474,10 @@ def flashrnn_embedding_fwd(table, tokens, scale=1.0, dtype=None, out=None, strea
 def flashrnn_embedding_bwd(tokens, dout, vocab, scale=1.0, dtable=None, accumulate=False, workspace=None, stream=None):
     """dtable[v] = scale * sum of dout over the places of word v; dtable[vocab, width] f32.  accumulate: added to the dtable passed in, rows of words that do not
     occur untouched.  The same result on every run."""
+    if _native is not None and stream is None and dtable is not None:
+        rc = _native.embedding_bwd(tokens, dout, vocab, scale, dtable, accumulate, workspace)
+        if rc <= 0:
+            return _done(rc, "flashrnn_embedding_bwd", dtable)
     H = dout.shape[-1]
     _chk(dout, (*tokens.shape, H), dout.dtype, "dout")
     _chk(tokens, tokens.shape, tokens.dtype, "tokens")
@@ -521,6 +538,12 @@ def _norm_desc(x, weight, bias, io, dx, eps):
 def flashrnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, dtype=None, save_for_backward=True, y=None, mean=None, rstd=None, stream=None):
     """Layer norm over the last axis of x, in x's type or in `dtype`.  weight, bias: [D], or [NH, D] for x[..., NH, D] (head by head), or None.  x may have one leading
     axis that is not dense, as the hidden states states[1:, 0] of a flashrnn_fwd call.  Returns (y, mean, rstd), the last two f32 of x.shape[:-1], or None, None."""
+    if _native is not None and stream is None and y is not None and (mean is not None and rstd is not None or not save_for_backward):
+        if not save_for_backward:
+            mean = rstd = None
+        rc = _native.layer_norm_fwd(x, weight, bias, eps, y, mean, rstd)
+        if rc <= 0:
+            return _done(rc, "flashrnn_layer_norm_fwd", (y, mean, rstd))
     if y is None:
         y = torch.empty(x.shape, dtype=x.dtype if dtype is None else dtype, device=x.device)
     _chk(y, x.shape, y.dtype, "y")
@@ -542,6 +565,11 @@ def flashrnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, dtype=None, sav
 def flashrnn_layer_norm_bwd(dy, x, mean, rstd, weight=None, dtype=None, param_grads=True, out=None, workspace=None, stream=None):
     """Gradient of flashrnn_layer_norm_fwd.  Returns (dx, dweight, dbias): dx dense, in dy's type or in `dtype`; the others f32 in weight's shape ([D] without a weight), or None
     where param_grads is false.  `out` may pass preallocated (dx, dweight, dbias)."""
+    if _native is not None and stream is None and out is not None:
+        dx, dweight, dbias = out if param_grads else (out[0], None, None)
+        rc = _native.layer_norm_bwd(dy, x, mean, rstd, weight, dx, dweight, dbias, workspace)
+        if rc <= 0:
+            return _done(rc, "flashrnn_layer_norm_bwd", (dx, dweight, dbias))
     _chk(dy, x.shape, dy.dtype, "dy")
     _chk(mean, x.shape[:-1], torch.float32, "mean")
     _chk(rstd, x.shape[:-1], torch.float32, "rstd")
@@ -581,6 +609,12 @@ def flashrnn_cross_entropy(logits, targets, dloss=None, grad_scale=1.0, gradient
     """Cross entropy of every row of logits[rows, classes] against targets[rows] (int64 or int32; outside the classes: ignored, loss 0), and in the same pass the
     gradient of sum(grad_scale * dloss * loss).  dlogits may be `logits` itself; lse, where passed, takes the rows' log of the sum of exponentials.
     Returns (loss f32[rows], dlogits in logits' type, or None where gradient is false)."""
+    if _native is not None and stream is None and loss is not None and (dlogits is not None or not gradient):
+        if not gradient:
+            dlogits = None
+        rc = _native.cross_entropy(logits, targets, dloss, grad_scale, loss, lse, dlogits)
+        if rc <= 0:
+            return _done(rc, "flashrnn_cross_entropy", (loss, dlogits))
     N, V = logits.shape
     stride = _matrix(logits, (N, V), logits.dtype, "logits")
     _chk(targets, (N,), targets.dtype, "targets")
@@ -605,6 +639,10 @@ def flashrnn_cross_entropy(logits, targets, dloss=None, grad_scale=1.0, gradient
 def flashrnn_grad_clip(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
     """The norm over all values of the tensors in `grads` (bf16 or f32, any mix), and the tensors scaled down so that it is max_norm at most: in place, or into the
     tensors of `out`.  max_norm = inf computes the norm alone (and copies into `out`).  Returns norm f32[1]."""
+    if _native is not None and stream is None and norm is not None:
+        rc = _native.grad_clip(grads, max_norm, out, norm, workspace, out is not None or max_norm != float("inf"))
+        if rc <= 0:
+            return _done(rc, "flashrnn_grad_clip", norm)
     grads = list(grads)
     n = len(grads)
     to = grads if out is None else list(out)

@@ -561,3 +561,93 @@ def test_operators_in_a_graph():
         got = [s[k].clone() for k in ("x", "y", "loss", "dy", "dx", "dweight", "dbias", "dtable", "norm")]
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, _all_of_them(new)))
+
+
+# ---- the native part of the binding ------------------------------------------------------------------------------------------------------------
+def _calls():
+    """Calls with every buffer passed, so that the native module may take them, and changes to them that it hands back."""
+    gen = _gen(11)
+    w, b = _normal(gen, 5, 16), _normal(gen, 5, 16)
+    states = _normal(gen, 4, 2, 3, 5, 16)
+    lead = (3, 3, 5)
+    tokens, table, logits = torch.tensor([[1, 5, -1], [9, 1, 3]]).cuda(), _normal(gen, 9, 16), _normal(gen, 6, 9)
+    z = lambda *shape, dtype=F32: torch.zeros(shape, dtype=dtype, device="cuda")
+    h, t6 = states[1:, 0], tokens.reshape(-1)
+    norm = dict(x=h, weight=w, bias=b, y=z(3, 3, 5, 16, dtype=BF16), mean=z(*lead), rstd=z(*lead))
+    _, mean, rstd = api.flashrnn_layer_norm_fwd(h, w, b)
+    grad = dict(dy=_normal(gen, 3, 3, 5, 16, dtype=BF16), x=h, mean=mean, rstd=rstd, weight=w, out=(z(3, 3, 5, 16, dtype=BF16), z(5, 16), z(5, 16)))
+    loss = dict(logits=logits, targets=t6, dloss=_normal(gen, 6), grad_scale=0.5, loss=z(6), lse=z(6), dlogits=z(6, 9))
+    wide = _normal(gen, 6, 14)
+    embed = dict(table=table, tokens=tokens, scale=2.0, out=z(2, 3, 16))
+    dembed = dict(tokens=tokens, dout=_normal(gen, 2, 3, 16), vocab=9, scale=2, dtable=z(9, 16))
+    clip = dict(grads=[_normal(gen, 7), _normal(gen, 3, 4, dtype=BF16)], max_norm=0.5, out=[z(7), z(3, 4, dtype=BF16)], norm=z(1))
+    strided = lambda t: t.transpose(0, -1).contiguous().transpose(0, -1)
+    return [
+        (api.flashrnn_embedding_fwd, embed, [dict(out=z(2, 3, 16, dtype=BF16)), dict(tokens=tokens.int()), dict(table=torch.nn.Parameter(table)), dict(scale=3), dict(out=None), dict(scale=True), dict(scale=torch.tensor(2.0))],
+         [dict(tokens=tokens.float()), dict(tokens=tokens.t()), dict(out=z(3, 2, 16)), dict(out=z(2, 3, 15)), dict(table=strided(table)), dict(table=table.double()), dict(table=table[0]),
+          dict(tokens=tokens.cpu()), dict(table=table[:0])]),
+        (api.flashrnn_embedding_bwd, dembed, [dict(accumulate=True), dict(tokens=tokens.int()), dict(workspace=z(100000)), dict(dtable=None), dict(vocab=torch.tensor(9))],
+         [dict(vocab=8), dict(vocab=2 ** 70), dict(vocab=-1), dict(dtable=z(9, 15)), dict(dout=z(3, 2, 16)), dict(workspace=z(1)), dict(dtable=z(9, 16, dtype=BF16)), dict(dout=dembed["dout"].double())]),
+        (api.flashrnn_layer_norm_fwd, norm, [dict(weight=None), dict(bias=None), dict(weight=None, bias=None), dict(x=h.contiguous()), dict(save_for_backward=False), dict(eps=1), dict(y=None), dict(mean=None),
+                                             dict(x=states[::2, 1], y=z(2, 3, 5, 16), mean=z(2, 3, 5), rstd=z(2, 3, 5))],
+         [dict(x=strided(h)), dict(weight=w[:4]), dict(bias=b.bfloat16()), dict(weight=w[0], bias=b), dict(y=z(3, 3, 5, 15)), dict(mean=z(3, 3)), dict(eps=-1.0), dict(eps=float("nan")),
+          dict(x=h.half()), dict(weight=w.t()), dict(x=h.cpu()), dict(rstd=z(*lead, dtype=BF16))]),
+        (api.flashrnn_layer_norm_bwd, grad, [dict(weight=None, out=(z(3, 3, 5, 16), z(16), z(16))), dict(param_grads=False), dict(out=(z(3, 3, 5, 16), None, z(5, 16))), dict(workspace=z(100000)), dict(out=None),
+                                             dict(x=h.contiguous())],
+         [dict(dy=grad["dy"][:2]), dict(mean=mean[:2]), dict(rstd=rstd.double()), dict(workspace=z(1)), dict(out=(z(3, 3, 5, 16), z(16), z(5, 16))), dict(weight=w[:4]), dict(x=strided(h))]),
+        (api.flashrnn_cross_entropy, loss, [dict(dloss=None), dict(lse=None), dict(gradient=False), dict(dlogits=None), dict(targets=t6.int()), dict(logits=wide[:, 2:11]), dict(dlogits=z(6, 12)[:, 1:10]), dict(grad_scale=2)],
+         [dict(targets=t6[:5]), dict(targets=t6.float()), dict(logits=strided(logits)), dict(dlogits=z(6, 9, dtype=BF16)), dict(dlogits=z(1, 9).expand(6, 9)), dict(loss=z(5)), dict(lse=z(6, dtype=BF16)),
+          dict(dloss=z(6).double()), dict(logits=logits[0]), dict(logits=logits.half())]),
+        (api.flashrnn_grad_clip, clip, [dict(max_norm=1e9), dict(max_norm=float("inf")), dict(grads=tuple(clip["grads"])), dict(workspace=z(100000)), dict(max_norm=1), dict(norm=None),
+                                        dict(grads=[clip["out"][0], clip["out"][1]], out=None)],
+         [dict(out=clip["out"][:1]), dict(out=[clip["out"][0], z(3, 4)]), dict(grads=[z(7), z(3, 4).t()]), dict(grads=[z(7), z(3, 4).double()]), dict(norm=z(2)), dict(max_norm=-1.0), dict(workspace=z(1)),
+          dict(max_norm=float("nan"))]),
+    ]
+
+
+def _outcome(fn, kw):
+    """What a call returns and leaves in its buffers, or what it raises."""
+    flat = lambda v: [v] if torch.is_tensor(v) else [t for x in v for t in flat(x)] if isinstance(v, (list, tuple)) else []
+    kw = {k: (v.clone() if torch.is_tensor(v) and k in ("out", "dtable", "y", "mean", "rstd", "loss", "lse", "dlogits", "norm") and v.is_contiguous() and fn is not api.flashrnn_layer_norm_bwd else v)
+          for k, v in kw.items()}
+    if fn is api.flashrnn_grad_clip and kw["out"] is None:
+        kw["grads"] = [g.clone() for g in kw["grads"]]
+    try:
+        result = fn(**kw)
+    except Exception as e:
+        return type(e).__name__, str(e)
+    torch.cuda.synchronize()
+    return [t.clone().cpu() for t in flat(result) + flat([kw.get(k) for k in ("out", "lse", "grads") if kw.get(k) is not None])]
+
+
+def test_native_calls_and_calls_through_python_give_and_refuse_the_same(monkeypatch):
+    api.lib()
+    assert api._native is not None
+    results = {}
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(api, "_native", None)
+        results[native] = []
+        for fn, base, fine, refused in _calls():
+            for i, change in enumerate([{}] + fine + refused):
+                got = _outcome(fn, dict(base, **change))
+                assert isinstance(got, tuple) == (i > len(fine)), (fn.__name__, change, got)
+                results[native].append((fn.__name__, i, got))
+    for (name, i, a), (_, _, b) in zip(results[True], results[False]):
+        assert type(a) is type(b), (name, i, a, b)
+        assert a == b if isinstance(a, tuple) else len(a) == len(b) and all(torch.equal(p, q) for p, q in zip(a, b)), (name, i)
+
+
+def test_plain_calls_are_made_by_the_native_module():
+    api.lib()
+    (_, embed, *_), (_, dembed, *_), (_, norm, *_), (_, grad, *_), (_, loss, *_), (_, clip, *_) = _calls()
+    n = api._native
+    assert n.embedding_fwd(embed["table"], embed["tokens"], 2.0, embed["out"]) == 0
+    assert n.embedding_bwd(dembed["tokens"], dembed["dout"], 9, 2, dembed["dtable"], False, None) == 0
+    assert n.layer_norm_fwd(norm["x"], norm["weight"], norm["bias"], 1e-5, norm["y"], norm["mean"], norm["rstd"]) == 0
+    assert n.layer_norm_bwd(grad["dy"], grad["x"], grad["mean"], grad["rstd"], grad["weight"], *grad["out"], None) == 0
+    assert n.cross_entropy(loss["logits"], loss["targets"], None, 0.5, loss["loss"], None, loss["dlogits"]) == 0
+    assert n.grad_clip(clip["grads"], 0.5, clip["out"], clip["norm"], None, True) == 0
+    for f in (n.embedding_fwd, n.embedding_bwd, n.layer_norm_fwd, n.layer_norm_bwd, n.cross_entropy, n.grad_clip):
+        assert f() == 1 and f(*range(9)) == 1
+    torch.cuda.synchronize()
