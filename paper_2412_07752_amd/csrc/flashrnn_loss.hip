@@ -17,7 +17,7 @@ struct Problem {
     float *loss, *lse;
     void* dlogits;
     size_t rows, stride, to_stride;
-    int classes, index64, stream;
+    int classes, index64;
     float scale;
 };
 __device__ __forceinline__ int64_t target_of(const Problem& p, size_t row) { return p.index64 ? ((const int64_t*)p.targets)[row] : ((const int32_t*)p.targets)[row]; }
@@ -25,8 +25,9 @@ __device__ __forceinline__ int64_t target_of(const Problem& p, size_t row) { ret
 __device__ __forceinline__ float exp_below(float x, float top) { return fast_exp2((x - top) * kLog2e); }
 
 // Groups of L threads hold a row as K chunks of V values each, laid out as RowPart says.  Up to 7 chunks (57344 classes in bf16) the kernel keeps to 64 registers, so that a CU holds two
-// workgroups of 1024 threads and one's loads and stores run beside the other's arithmetic: 16384 x 50304 in bf16 565 us (5.8 TB/s), with one workgroup 653; eight chunks do not fit.
-template <typename X, int L, int K>
+// workgroups of 1024 threads and one's loads and stores run beside the other's arithmetic: 16384 x 50304 in bf16 565 us, with one workgroup 653; eight chunks do not fit.
+// STREAM: the gradient goes past the caches (536 us, 6.1 TB/s), decided when compiled because the 64 registers do not hold both stores.
+template <typename X, int L, int K, bool STREAM>
 __global__ __launch_bounds__(threads_of<L>(), L == 1024 && K <= 7 ? 8 : 1) void loss_rows_kernel(Problem p) {
     constexpr int V = 16 / sizeof(X), NT = threads_of<L>(), PER = NT / L;
     __shared__ float slots[2][NT / kWave];
@@ -94,14 +95,14 @@ __global__ __launch_bounds__(threads_of<L>(), L == 1024 && K <= 7 ? 8 : 1) void 
             if (p.dlogits && part.stores(k)) {
                 Chunk<X, V> c;
                 c.put(g);
-                c.store((X*)p.dlogits + row * p.to_stride + part.at[k], p.stream);
+                c.store((X*)p.dlogits + row * p.to_stride + part.at[k], STREAM);
             }
         }
     }
 }
 
 // Rows that no group's registers hold, and rows shorter than a chunk: read twice, the sum kept up with a running maximum.
-template <typename X, int NT>
+template <typename X, int NT, bool STREAM>
 __global__ __launch_bounds__(NT) void loss_long_kernel(Problem p) {
     constexpr int V = 16 / sizeof(X);
     __shared__ float slots[2][NT / kWave];
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(NT) void loss_long_kernel(Problem p) {
 #pragma unroll
             for (int i = 0; i < V; ++i) g[i] = grad(c.get(i), at + i);
             c.put(g);
-            c.store(dx + at, p.stream);
+            c.store(dx + at, STREAM);
         }
         if (tail < p.classes) store_value(dx + tail, grad(load_value(x + tail), tail));
     }
@@ -181,7 +182,8 @@ extern "C" int flashrnn_cross_entropy(const flashrnn_cross_entropy_desc_t* d, co
         return FLASHRNN_ERR_UNSUPPORTED;
     const size_t rows = (size_t)d->rows;
     const Problem p{logits, targets, (const float*)dloss, (float*)loss, (float*)lse, dlogits, rows, (size_t)d->logits_stride, (size_t)d->dlogits_stride, d->classes,
-                    d->index_dtype == FLASHRNN_I64, rows * d->classes * e > kStreamBytes, d->grad_scale};
+                    d->index_dtype == FLASHRNN_I64, d->grad_scale};
+    const bool past_caches = rows * d->classes * e > kStreamBytes;
     const hipStream_t stream = (hipStream_t)hip_stream;
     return with_io_type(d->io_dtype, [&](auto* xt) {
         using X = std::remove_pointer_t<decltype(xt)>;
@@ -189,13 +191,16 @@ extern "C" int flashrnn_cross_entropy(const flashrnn_cross_entropy_desc_t* d, co
         int rc = FLASHRNN_OK;
         auto launch = [&](auto s) {
             constexpr int L = decltype(s)::L, K = decltype(s)::K, NT = threads_of<L>(), PER = NT / L;
-            hipLaunchKernelGGL((loss_rows_kernel<X, L, K>), dim3(row_blocks((rows + PER - 1) / PER)), dim3(NT), 0, stream, p);
+            const dim3 grid(row_blocks((rows + PER - 1) / PER));
+            if (past_caches) hipLaunchKernelGGL((loss_rows_kernel<X, L, K, true>), grid, dim3(NT), 0, stream, p);
+            else hipLaunchKernelGGL((loss_rows_kernel<X, L, K, false>), grid, dim3(NT), 0, stream, p);
             rc = launch_status();
         };
         const int chunks = (d->classes + V - 1) / V;
         if (d->classes >= V && (with_shape(chunks, launch) || with_long_shape(chunks, launch))) return rc;
-        if (d->classes < V) hipLaunchKernelGGL((loss_long_kernel<X, kWave>), dim3(row_blocks(rows)), dim3(kWave), 0, stream, p);
-        else hipLaunchKernelGGL((loss_long_kernel<X, 1024>), dim3(row_blocks(rows)), dim3(1024), 0, stream, p);
+        if (d->classes < V) hipLaunchKernelGGL((loss_long_kernel<X, kWave, false>), dim3(row_blocks(rows)), dim3(kWave), 0, stream, p);
+        else if (past_caches) hipLaunchKernelGGL((loss_long_kernel<X, 1024, true>), dim3(row_blocks(rows)), dim3(1024), 0, stream, p);
+        else hipLaunchKernelGGL((loss_long_kernel<X, 1024, false>), dim3(row_blocks(rows)), dim3(1024), 0, stream, p);
         return launch_status();
     });
 }

@@ -122,11 +122,11 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_rows_kernel(Rows r
 
 // The gradient, rows in registers as above: dx from the row's two sums, and every thread's part of dweight and dbias in its registers over all rows that its group takes.
 // At the end the groups of a workgroup that share a row of the weights meet in LDS and their sum, in the order of the groups, is one row of partial sums; with more
-// rows of weights than groups every group writes its own.  sums: [dweight, dbias][strips][groups][width], a strip for every workgroup, or for every `groups` groups of threads.
+// rows of weights than groups every group writes its own.  dweight, dbias: [strips][groups][width] each, a strip for every workgroup, or for every `groups` groups of threads; or null.
 template <typename X, typename Y, int V, int L, int K>
 __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(Rows r, const Y* __restrict__ dy, const X* __restrict__ x, const void* __restrict__ weight,
                                                                               bool weight_bf16, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-                                                                              void* __restrict__ dx, bool dx_bf16, bool stream, float* __restrict__ sums, size_t sum_rows) {
+                                                                              void* __restrict__ dx, bool dx_bf16, bool stream, float* __restrict__ dweight, float* __restrict__ dbias) {
     constexpr int NT = threads_of<L>(), PER = NT / L;
     __shared__ float slots[2][2][NT / kWave];
     __shared__ float merge[PER > 1 ? NT * K * V : 1];
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(R
             }
         }
     }
-    if (!sums) return;
+    if (!dweight && !dbias) return;
     const bool shared = r.groups <= PER;
     const uint32_t to = shared ? blockIdx.x * r.groups + first % r.groups : first;
 #pragma unroll
@@ -231,8 +231,9 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(R
 #pragma unroll
                         for (int i = 0; i < V; ++i) v[k][i] += merge[(k * V + i) * NT + other * L + l];
         }
-        if (!shared || group < r.groups) {
-            float* out = sums + (which * sum_rows + to) * r.width;
+        float* out = which ? dbias : dweight;
+        if (out && (!shared || group < r.groups)) {
+            out += (size_t)to * r.width;
 #pragma unroll
             for (int k = 0; k < K; ++k)
                 if (part.stores(k)) {
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(R
 }
 
 // dweight and dbias from partial sums [dweight, dbias][strips][columns]: a wave adds up every kSumWaves-th strip of 64 columns, in order, then the waves meet
-constexpr int kSumWaves = 16;
+constexpr int kSumWaves = 16, kSumAhead = 8;   // (loads on their way)
 __global__ __launch_bounds__(kSumWaves * kWave) void layer_norm_sum_strips_kernel(const float* __restrict__ part, size_t columns, int strips, float* __restrict__ dweight,
                                                                                  float* __restrict__ dbias) {
     __shared__ float lds[kSumWaves][kWave];
@@ -256,12 +257,12 @@ __global__ __launch_bounds__(kSumWaves * kWave) void layer_norm_sum_strips_kerne
     const float* p = part + (size_t)blockIdx.y * strips * columns + (col < columns ? col : columns - 1);
     float s = 0.f;
     int i = w;
-    for (; i + 7 * kSumWaves < strips; i += 8 * kSumWaves) {   // eight loads on their way
-        float v[8];
+    for (; i + (kSumAhead - 1) * kSumWaves < strips; i += kSumAhead * kSumWaves) {
+        float v[kSumAhead];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = p[(size_t)(i + u * kSumWaves) * columns];
+        for (int u = 0; u < kSumAhead; ++u) v[u] = p[(size_t)(i + u * kSumWaves) * columns];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) s += v[u];
+        for (int u = 0; u < kSumAhead; ++u) s += v[u];
     }
     for (; i < strips; i += kSumWaves) s += p[(size_t)i * columns];
     lds[w][lane] = s;
@@ -291,12 +292,14 @@ inline unsigned blocks_for(size_t rows, int per, int groups, unsigned most) {
 }
 
 // launch of the gradient with rows in registers; blocks = 0: none
+// Up to so many rows per group one workgroup does it all and writes dweight and dbias itself, a launch less: 60 rows of 72 values, two a group, 9.0 us and 10.3; 22 of 920, three a group, 9.0 and 8.5.
+constexpr uint32_t kAloneRounds = 2;
 struct GradPlan {
     unsigned blocks;
     size_t sum_rows;   // rows of partial sums
 };
 inline GradPlan grad_plan(const Rows& r, int per, int threads) {
-    GradPlan p{blocks_for(r.count, per, r.groups, kMostGradThreads / threads), 0};
+    GradPlan p{r.count <= kAloneRounds * per && per % r.groups == 0 ? 1 : blocks_for(r.count, per, r.groups, kMostGradThreads / threads), 0};
     if (r.groups > per) {   // whole strips: workgroups beyond the rows write zeros
         const size_t unit = lcm_of(r.groups, per) / per;
         p.blocks = unit > (1u << 20) ? 0 : (unsigned)((p.blocks + unit - 1) / unit * unit);
@@ -467,11 +470,12 @@ int flashrnn_layer_norm_bwd(const flashrnn_layer_norm_desc_t* d, const void* dy,
         strips = (int)(p.sum_rows / r.groups);
         hipLaunchKernelGGL((layer_norm_grad_rows_kernel<X, Y, decltype(v)::value, L, K>), dim3(p.blocks), dim3(NT), 0, stream, r, (const Y*)dy, (const X*)x, weight,
                            d->param_dtype == FLASHRNN_BF16, (const float*)mean, (const float*)rstd, dx, d->dx_dtype == FLASHRNN_BF16,
-                           rows * d->width * type_size(d->dx_dtype) > kStreamBytes, params ? (float*)workspace : nullptr, p.sum_rows);
+                           rows * d->width * type_size(d->dx_dtype) > kStreamBytes, strips == 1 ? (float*)dweight : params ? (float*)workspace : nullptr,
+                           strips == 1 ? (float*)dbias : params ? (float*)workspace + p.sum_rows * d->width : nullptr);
         rc = launch_status();
     });
     if (taken) {
-        if (rc != FLASHRNN_OK || !params) return rc;
+        if (rc != FLASHRNN_OK || !params || strips == 1) return rc;
         hipLaunchKernelGGL(layer_norm_sum_strips_kernel, dim3((unsigned)((columns + kWave - 1) / kWave), 2), dim3(kSumWaves * kWave), 0, stream, (const float*)workspace, columns,
                            strips, (float*)dweight, (float*)dbias);
         return launch_status();

@@ -53,18 +53,28 @@ template <typename T, int V> struct Chunk {
             }
         }
     }
-    // stream: past the caches, for outputs that these cannot hold
+    // stream: past the caches, for outputs that these cannot hold.  (The empty asm keeps the compiler from joining the two stores into one that is neither.)
     __device__ __forceinline__ void store(T* p, bool stream = false) const {
         if constexpr (W == 2) {
             const i32x2_any a = {(int)w[0], (int)w[1]};
-            if (stream) __builtin_nontemporal_store(a, (i32x2_any*)p);
-            else *(i32x2_any*)p = a;
+            if (stream) {
+                asm volatile("");
+                __builtin_nontemporal_store(a, (i32x2_any*)p);
+                asm volatile("");
+            } else {
+                *(i32x2_any*)p = a;
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < W / 4; ++i) {
                 const i32x4_any a = {(int)w[4 * i], (int)w[4 * i + 1], (int)w[4 * i + 2], (int)w[4 * i + 3]};
-                if (stream) __builtin_nontemporal_store(a, (i32x4_any*)p + i);
-                else ((i32x4_any*)p)[i] = a;
+                if (stream) {
+                    asm volatile("");
+                    __builtin_nontemporal_store(a, (i32x4_any*)p + i);
+                    asm volatile("");
+                } else {
+                    ((i32x4_any*)p)[i] = a;
+                }
             }
         }
     }
