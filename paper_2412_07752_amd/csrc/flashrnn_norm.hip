@@ -8,8 +8,8 @@ namespace {
 // Workgroups of a forward call: 65536 x 8 x 256 states take 161 us with 768 workgroups of 256 threads, 162 with 2048, 148 with 8192 and 160 with one row for every
 // group of threads.
 constexpr unsigned kMostThreads = 8192 * 256;
-// ... and of a gradient, whose workgroups each leave partial sums of dweight and dbias: 16384 x 768 values in bf16 take 19.8 us with 512 workgroups of 256 threads, 23 with 768,
-// 25 with 1024 and 32 with 2048; 65536 x 8 x 256 states 210, 218, 234 and 236.
+// ... and of a gradient, whose workgroups each leave partial sums of dweight and dbias: 16384 x 768 values in bf16 take 20.2 us with 256 workgroups of 256 threads, 18.6 with 512, 19.2 with 768
+// and 20.0 with 1024; 65536 x 8 x 256 states 191, 197, 213 and 220, 65536 x 2048 in bf16 237, 158, 150 and 154.
 constexpr unsigned kMostGradThreads = 512 * 256;
 constexpr int kMaxStrips = 256;   // workgroups that add up the gradients of weight and bias, each over a strip of rows
 
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(R
                                                                               void* __restrict__ dx, bool dx_bf16, bool stream, float* __restrict__ dweight, float* __restrict__ dbias) {
     constexpr int NT = threads_of<L>(), PER = NT / L;
     __shared__ float slots[2][2][NT / kWave];
-    __shared__ float merge[PER > 1 ? NT * K * V : 1];
+    __shared__ float merge[PER > 1 ? 2 * NT * K * V : 1];
     const int l = threadIdx.x % L, group = threadIdx.x / L;
     const uint32_t stride = gridDim.x * PER, first = blockIdx.x * PER + group;
     const uint32_t lead = L <= kWave ? blockIdx.x * PER + threadIdx.x / kWave * (kWave / L) : first;
@@ -212,36 +212,52 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(R
         }
     }
     if (!dweight && !dbias) return;
-    const bool shared = r.groups <= PER;
-    const uint32_t to = shared ? blockIdx.x * r.groups + first % r.groups : first;
+    if (PER > 1 && r.groups <= PER) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                merge[(k * V + i) * NT + threadIdx.x] = dw[k][i];
+                merge[((K + k) * V + i) * NT + threadIdx.x] = db[k][i];
+            }
+        __syncthreads();
+        // every thread some of the sums: a chunk of one thread of a group, or, where these are fewer than the threads, a value of one
+        constexpr int N = 2 * L * K >= NT ? V : 1, kEach = L * K * V / N;
+        const int half = r.groups * kEach;
+        for (int o = threadIdx.x; o < 2 * half; o += NT) {
+            const int which = o >= half, rest = o - (which ? half : 0), row = rest / kEach, of = rest % L, value = rest % kEach / L * N, begin = (value / V * L + of) * V;
+            float* out = which ? dbias : dweight;
+            if (!out || begin >= r.width) continue;
+            const float* from = merge + (which * K * V + value) * NT + of;
+            float sum[N] = {};
+            for (int g = row; g < PER; g += r.groups)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] += from[i * NT + g * L];
+            const uint32_t to = blockIdx.x * r.groups + (r.groups == 1 ? 0 : (blockIdx.x * PER + row) % r.groups);
+            out += (size_t)to * r.width + (begin < r.width - V ? begin : r.width - V) + value % V;
+            if constexpr (N == V) {
+                Chunk<float, V> c;
+                c.put(sum);
+                c.store(out);
+            } else {
+                *out = sum[0];
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         float(&v)[K][V] = which ? db : dw;
-        if (PER > 1 && shared) {
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) merge[(k * V + i) * NT + threadIdx.x] = v[k][i];
-            __syncthreads();
-            if (group < r.groups)
-                for (int other = group + r.groups; other < PER; other += r.groups)
-#pragma unroll
-                    for (int k = 0; k < K; ++k)
-#pragma unroll
-                        for (int i = 0; i < V; ++i) v[k][i] += merge[(k * V + i) * NT + other * L + l];
-        }
         float* out = which ? dbias : dweight;
-        if (out && (!shared || group < r.groups)) {
-            out += (size_t)to * r.width;
+        if (!out) continue;
+        out += (size_t)first * r.width;
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (part.stores(k)) {
-                    Chunk<float, V> c;
-                    c.put(v[k]);
-                    c.store(out + part.at[k]);
-                }
-        }
+        for (int k = 0; k < K; ++k)
+            if (part.stores(k)) {
+                Chunk<float, V> c;
+                c.put(v[k]);
+                c.store(out + part.at[k]);
+            }
     }
 }
 
@@ -292,8 +308,9 @@ inline unsigned blocks_for(size_t rows, int per, int groups, unsigned most) {
 }
 
 // launch of the gradient with rows in registers; blocks = 0: none
-// Up to so many rows per group one workgroup does it all and writes dweight and dbias itself, a launch less: 60 rows of 72 values, two a group, 9.0 us and 10.3; 22 of 920, three a group, 9.0 and 8.5.
-constexpr uint32_t kAloneRounds = 2;
+// Up to so many rows per group one workgroup does it all and writes dweight and dbias itself, a launch less: 60 rows of 72 values, two a group, 5.5 us and 9.0; 22 of 920, three a group, 7.8 and
+// 8.6; 200 of 72, seven a group, 9.4 and 9.0.
+constexpr uint32_t kAloneRounds = 4;
 struct GradPlan {
     unsigned blocks;
     size_t sum_rows;   // rows of partial sums
@@ -379,13 +396,19 @@ int strips_of(const flashrnn_layer_norm_desc_t* d) {
     return tokens < kMaxStrips ? (tokens ? (int)tokens : 1) : kMaxStrips;
 }
 
-// calls f(X*, Y*, V, shape) for a gradient whose rows fit in registers
+// Calls f(X*, Y*, V, shape) for a gradient whose rows fit in registers.  Chunks of four values also in bf16, as long as a workgroup's registers hold the row: with eight the sums of
+// dweight and dbias leave a SIMD one or two waves (16384 x 768 values 18.6 us and 21.0, 65536 x 256 25 and 32, 65536 x 2048 157 and 152).
 template <typename F> void with_grad_shape(const flashrnn_layer_norm_desc_t* d, F&& f) {
     if (d->width < 8) return;
     with_io_type(d->x_dtype, [&](auto* xt) {
         return with_io_type(d->io_dtype, [&](auto* yt) {
-            constexpr int V = sizeof(*xt) == 2 && sizeof(*yt) == 2 ? 8 : 4;
-            return (int)with_shape((d->width + V - 1) / V, [&](auto s) { f(xt, yt, Int<V>{}, s); });
+            if (with_shape((d->width + 3) / 4, [&](auto s) { f(xt, yt, Int<4>{}, s); })) return 0;
+            if constexpr (sizeof(*xt) == 2 && sizeof(*yt) == 2) {   // rows of more than 8192 values
+                const int chunks = (d->width + 7) / 8;
+                if (chunks <= 512 * 3) f(xt, yt, Int<8>{}, Shape<512, 3>{});
+                else if (chunks <= 512 * 4) f(xt, yt, Int<8>{}, Shape<512, 4>{});
+            }
+            return 0;
         });
     });
 }
