@@ -34,7 +34,7 @@ __global__ __launch_bounds__(threads_of<L>(), L == 1024 && K <= 7 ? 8 : 1) void 
     const int l = threadIdx.x % L;
     const RowPart<L, K, V> part(l, p.classes);
     for (size_t base = (size_t)blockIdx.x * PER + (L <= kWave ? threadIdx.x / kWave * (kWave / L) : 0); base < p.rows; base += (size_t)gridDim.x * PER) {
-        const size_t row = L <= kWave ? base + threadIdx.x % kWave / L : base;
+        const size_t row = base + (L <= kWave ? threadIdx.x % kWave / L : threadIdx.x / L);
         const bool there = row < p.rows;
         const int64_t t = there ? target_of(p, row) : -1;
         const bool counts = t >= 0 && t < p.classes;
@@ -197,7 +197,7 @@ extern "C" int flashrnn_cross_entropy(const flashrnn_cross_entropy_desc_t* d, co
             rc = launch_status();
         };
         const int chunks = (d->classes + V - 1) / V;
-        if (d->classes >= V && (with_shape(chunks, launch) || with_long_shape(chunks, launch))) return rc;
+        if (d->classes >= V && (with_shape<false>(chunks, launch) || with_long_shape(chunks, launch))) return rc;
         if (d->classes < V) hipLaunchKernelGGL((loss_long_kernel<X, kWave, false>), dim3(row_blocks(rows)), dim3(kWave), 0, stream, p);
         else if (past_caches) hipLaunchKernelGGL((loss_long_kernel<X, 1024, true>), dim3(row_blocks(rows)), dim3(1024), 0, stream, p);
         else hipLaunchKernelGGL((loss_long_kernel<X, 1024, false>), dim3(row_blocks(rows)), dim3(1024), 0, stream, p);

@@ -9,7 +9,7 @@ namespace {
 // group of threads.
 constexpr unsigned kMostThreads = 8192 * 256;
 // ... and of a gradient, whose workgroups each leave partial sums of dweight and dbias: 16384 x 768 values in bf16 take 20.2 us with 256 workgroups of 256 threads, 18.6 with 512, 19.2 with 768
-// and 20.0 with 1024; 65536 x 8 x 256 states 191, 197, 213 and 220, 65536 x 2048 in bf16 237, 158, 150 and 154.
+// and 20.0 with 1024; 65536 x 8 x 256 states 191, 197, 213 and 220, 65536 x 1200 in bf16 153, 100, 97 and 98.
 constexpr unsigned kMostGradThreads = 512 * 256;
 constexpr int kMaxStrips = 256;   // workgroups that add up the gradients of weight and bias, each over a strip of rows
 
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_rows_kernel(Rows r
     __shared__ float slots[2][NT / kWave];
     const int l = threadIdx.x % L;
     const uint32_t stride = gridDim.x * PER, first = blockIdx.x * PER + threadIdx.x / L;
-    const uint32_t lead = L <= kWave ? blockIdx.x * PER + threadIdx.x / kWave * (kWave / L) : first;   // the wave's first row
+    const uint32_t lead = blockIdx.x * PER + (L <= kWave ? threadIdx.x / kWave * (kWave / L) : 0);   // the first row of those that go through the loop together
     const RowPart<L, K, V> part(l, r.width);
     float w[K][V], b[K][V];
     const size_t own = (size_t)(first % r.groups) * r.width;
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(R
     __shared__ float merge[PER > 1 ? 2 * NT * K * V : 1];
     const int l = threadIdx.x % L, group = threadIdx.x / L;
     const uint32_t stride = gridDim.x * PER, first = blockIdx.x * PER + group;
-    const uint32_t lead = L <= kWave ? blockIdx.x * PER + threadIdx.x / kWave * (kWave / L) : first;
+    const uint32_t lead = blockIdx.x * PER + (L <= kWave ? threadIdx.x / kWave * (kWave / L) : 0);
     const RowPart<L, K, V> part(l, r.width);
     float w[K][V], dw[K][V], db[K][V];
 #pragma unroll
@@ -192,12 +192,13 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(R
                 slots[turn][1][threadIdx.x >> 6] = b;
             }
             __syncthreads();
-            a = slots[turn][0][0];
-            b = slots[turn][1][0];
+            const int own = group * (L / kWave);
+            a = slots[turn][0][own];
+            b = slots[turn][1][own];
 #pragma unroll
-            for (int i = 1; i < NT / kWave; ++i) {
-                a += slots[turn][0][i];
-                b += slots[turn][1][i];
+            for (int i = 1; i < L / kWave; ++i) {
+                a += slots[turn][0][own + i];
+                b += slots[turn][1][own + i];
             }
         }
         a /= n;
@@ -397,12 +398,12 @@ int strips_of(const flashrnn_layer_norm_desc_t* d) {
 }
 
 // Calls f(X*, Y*, V, shape) for a gradient whose rows fit in registers.  Chunks of four values also in bf16, as long as a workgroup's registers hold the row: with eight the sums of
-// dweight and dbias leave a SIMD one or two waves (16384 x 768 values 18.6 us and 21.0, 65536 x 256 25 and 32, 65536 x 2048 157 and 152).
+// dweight and dbias leave a SIMD one or two waves (16384 x 768 values 18.6 us and 21.0, 65536 x 256 25 and 32, 65536 x 2048 148 and 152).
 template <typename F> void with_grad_shape(const flashrnn_layer_norm_desc_t* d, F&& f) {
     if (d->width < 8) return;
     with_io_type(d->x_dtype, [&](auto* xt) {
         return with_io_type(d->io_dtype, [&](auto* yt) {
-            if (with_shape((d->width + 3) / 4, [&](auto s) { f(xt, yt, Int<4>{}, s); })) return 0;
+            if (with_shape<true>((d->width + 3) / 4, [&](auto s) { f(xt, yt, Int<4>{}, s); })) return 0;
             if constexpr (sizeof(*xt) == 2 && sizeof(*yt) == 2) {   // rows of more than 8192 values
                 const int chunks = (d->width + 7) / 8;
                 if (chunks <= 512 * 3) f(xt, yt, Int<8>{}, Shape<512, 3>{});
@@ -443,7 +444,7 @@ int flashrnn_layer_norm_fwd(const flashrnn_layer_norm_desc_t* d, const void* x, 
     if (d->width >= 8) with_io_type(d->x_dtype, [&](auto* xt) {
         using X = std::remove_pointer_t<decltype(xt)>;
         constexpr int V = 16 / sizeof(X);
-        return (int)with_shape((d->width + V - 1) / V, [&](auto s) {
+        return (int)with_shape<true>((d->width + V - 1) / V, [&](auto s) {
             constexpr int L = decltype(s)::L, K = decltype(s)::K, NT = threads_of<L>();
             const unsigned blocks = blocks_for(rows, NT / L, d->groups, kMostThreads / NT);
             if (!blocks) return;
