@@ -1,7 +1,7 @@
 // Embedding lookup and its gradient by sorted tokens (include/flashrnn.h).
 //
-// The gradient sorts the places by their word, stable, so that the places of a word stay in order: a radix sort, least significant digit first, by one workgroup in its LDS up to
-// kSmall places, by tiles of places on many workgroups beyond.  The table's rows are filled with zeros by the workgroups that the sort leaves idle.  Then groups of lanes
+// The gradient sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs, beyond by a radix sort, least significant digit
+// first, of tiles of places.  The table's rows are filled with zeros by the workgroups that the sort leaves idle.  Then groups of lanes
 // add up runs of consecutive sorted places and write the rows of the words that begin and end inside; what is left of a word at the ends of a run goes to the workspace, and a last kernel joins such pieces
 // in order.  Tokens outside the vocabulary sort behind all words.
 #include "flashrnn_rows.h"
@@ -12,12 +12,13 @@ namespace {
 
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
-constexpr int kSmall = 8192;       // places that one workgroup sorts
+// Places that are sorted by counting, the bits of their numbers, and those that a workgroup ranks.  Whole gradients of 80 columns: 11525 places 24.3 us by counting and 31.7 by tiles,
+// 16000 places 34.2 and 27.0.
+constexpr int kSmall = 12288, kSmallBits = 14, kRanked = 16;
 constexpr int kMaxTiles = 128;     // tiles of a larger sort
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / kWave;
-constexpr int kRounds = kSmall / kSortThreads;   // places per thread of the one workgroup
-constexpr int kTileRounds = 2;                   // ... of a tile at a time
+constexpr int kTileRounds = 2;     // places per thread of a tile at a time
 constexpr int kRows = 4;           // places that a group of lanes looks up at a time, where there are kManyWaves waves of places
 constexpr uint64_t kManyWaves = 16384;
 constexpr int kColumns = 4;        // columns a lane adds up: neighbours store whole cache lines of float32 (with eight, each store left every second 16 bytes out)
@@ -184,68 +185,38 @@ __device__ __forceinline__ uint32_t scan_digits(uint32_t v, uint32_t* lds) {
     return before + s - v;
 }
 
-// up to kSmall places, sorted by workgroup 0; the others fill
-__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const void* __restrict__ tokens, bool index64, uint32_t n, uint32_t vocab, int passes, int bits,
-                                                                  uint32_t* __restrict__ keys_out, uint32_t* __restrict__ places_out, Fill fill) {
-    __shared__ uint32_t keys[kSmall], counts[kSortWaves][kDigits], totals[kDigits / kWave];
-    __shared__ uint16_t places[kSmall];
-    if (blockIdx.x) return fill_zeros<kSortThreads>(fill, blockIdx.x - 1, gridDim.x - 1);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const uint32_t runs = (n + kWave - 1) / kWave, mine = (runs + kSortWaves - 1) / kSortWaves;   // runs of 64 places, `mine` of them in a row a wave
-    uint32_t key[kRounds], rank[kRounds];
-    uint16_t place[kRounds];
-#pragma unroll
-    for (int u = 0; u < kRounds; ++u) {
-        const uint32_t i = (w * mine + u) * kWave + lane;
-        const bool in = (uint32_t)u < mine && i < n;
-        key[u] = in ? key_of(tokens, index64, i, vocab) : ~0u;
-        place[u] = (uint16_t)i;
+// Up to kSmall places: every place's rank is the number of (word, place) pairs below its own, counted over all pairs.  A workgroup has the pairs in its LDS, as one number each, and ranks
+// kRanked places: lanes 16 apart and waves take different 64ths of the pairs.  4096 places are 17 M comparisons, two instructions each: 1 us of the whole chip, where a sort by one workgroup takes 15.
+// The workgroups beyond fill.  (Ranking and filling workgroups by turns: 8192 places among 32000 words 32.9 us instead of 34.8, among 300 words 23.7 instead of 20.5.)
+__global__ __launch_bounds__(kSortThreads) void rank_places_kernel(const void* __restrict__ tokens, bool index64, uint32_t n, uint32_t vocab, uint32_t* __restrict__ keys_out,
+                                                                   uint32_t* __restrict__ places_out, uint32_t blocks, Fill fill) {
+    constexpr uint32_t kParts = kSortThreads / kRanked;
+    __shared__ __align__(16) uint32_t pairs[kSmall + 4 * kParts];
+    __shared__ uint32_t ranks[kSortWaves][kRanked];
+    if (blockIdx.x >= blocks) return fill_zeros<kSortThreads>(fill, blockIdx.x - blocks, gridDim.x - blocks);
+    uint32_t part = (n + kParts - 1) / kParts;   // pairs of a 64th: whole reads of four, and 64ths that start in other banks
+    part = (part + 3) / 4 * 4;
+    if (part % 16 == 0) part += 4;
+    for (uint32_t i = threadIdx.x; i < part * kParts; i += kSortThreads) pairs[i] = i < n ? key_of(tokens, index64, i, vocab) << kSmallBits | i : ~0u;
+    __syncthreads();
+    const uint32_t lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = blockIdx.x * kRanked + lane % kRanked;
+    const uint32_t own = pairs[i < n ? i : n - 1], *from = pairs + (threadIdx.x / kRanked) * part;
+    uint32_t rank = 0;
+#pragma unroll 4
+    for (uint32_t j = 0; j < part; j += 4) {
+        const uint4 four = *(const uint4*)(from + j);
+        rank += (four.x < own) + (four.y < own) + (four.z < own) + (four.w < own);
     }
-    for (int pass = 0; pass < passes; ++pass) {
-        const int shift = pass * bits;
-        const uint32_t mask = (1u << bits) - 1;
-        for (int d = threadIdx.x; d < kSortWaves * kDigits; d += kSortThreads) counts[0][d] = 0;
-        __syncthreads();   // (and every wave has read the last pass's keys)
+    rank += __shfl_xor(rank, 16);
+    rank += __shfl_xor(rank, 32);
+    if (lane < kRanked) ranks[w][lane] = rank;
+    __syncthreads();
+    if (threadIdx.x >= kRanked || i >= n) return;
+    rank = 0;
 #pragma unroll
-        for (int u = 0; u < kRounds; ++u)
-            if ((uint32_t)u < mine) rank[u] = rank_in_wave(key[u] >> shift & mask, key[u] != ~0u, bits, counts[w]);
-        __syncthreads();
-        uint32_t total = 0;
-        if (threadIdx.x < kDigits)
-            for (int v = 0; v < kSortWaves; ++v) {
-                const uint32_t c = counts[v][threadIdx.x];
-                counts[v][threadIdx.x] = total;
-                total += c;
-            }
-        const uint32_t before = scan_digits(total, totals);
-        if (threadIdx.x < kDigits)
-            for (int v = 0; v < kSortWaves; ++v) counts[v][threadIdx.x] += before;
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kRounds; ++u)
-            if ((uint32_t)u < mine && key[u] != ~0u) {
-                const uint32_t to = counts[w][key[u] >> shift & mask] + rank[u];
-                keys[to] = key[u];
-                places[to] = place[u];
-            }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kRounds; ++u) {
-            const uint32_t i = (w * mine + u) * kWave + lane;
-            if ((uint32_t)u < mine && i < n) {
-                key[u] = keys[i];
-                place[u] = places[i];
-            }
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < kRounds; ++u) {
-        const uint32_t i = (w * mine + u) * kWave + lane;
-        if ((uint32_t)u < mine && i < n) {
-            keys_out[i] = key[u];
-            places_out[i] = place[u];
-        }
-    }
+    for (int v = 0; v < kSortWaves; ++v) rank += ranks[v][threadIdx.x];
+    keys_out[rank] = own >> kSmallBits;
+    places_out[rank] = i;
 }
 
 // One pass over more places: workgroup `tile` of `tiles` takes `span` of them.  keys == nullptr: the first digit, straight from the tokens.
@@ -481,7 +452,7 @@ int lanes_for(int chunks) {
 // How the gradient is laid out: the sort's passes and tiles, the runs, the workspace.
 struct Plan {
     int passes, bits;
-    uint32_t tiles, span;   // tiles = 0: the sort of one workgroup
+    uint32_t tiles, span;   // tiles = 0: sorted by counting
     int L, column_blocks;
     uint32_t run, runs;
     size_t keys[2], places[2], counts, flags, pieces, total;
@@ -495,7 +466,7 @@ Plan plan_of(const flashrnn_embedding_desc_t* d) {
     p.passes = (bits + kDigitBits - 1) / kDigitBits;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.tiles = p.span = 0;
-    if (n > kSmall) {
+    if (n > kSmall || (uint32_t)d->vocab >> (32 - kSmallBits)) {   // (word and place have to fit into 32 bits, with one number left above them all)
         const size_t step = kSortThreads * kTileRounds, steps = (n + step - 1) / step, each = (steps + kMaxTiles - 1) / kMaxTiles;
         p.span = (uint32_t)(each * step);
         p.tiles = (uint32_t)((n + p.span - 1) / p.span);
@@ -582,9 +553,9 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
     const uint32_t vocab = (uint32_t)d->vocab;
     uint32_t *keys = (uint32_t*)(ws + p.keys[0]), *places = (uint32_t*)(ws + p.places[0]);
     if (p.tiles == 0) {
-        const unsigned blocks = fill_to(vocab, kSortWaves);
-        hipLaunchKernelGGL(sort_small_kernel, dim3(1 + blocks), dim3(kSortThreads), 0, stream, tokens, d->index_dtype == FLASHRNN_I64, (uint32_t)n, vocab, p.passes, p.bits, keys, places,
-                           fill);
+        const unsigned fills = fill_to(vocab, kSortWaves), blocks = (unsigned)((n + kRanked - 1) / kRanked);
+        if (blocks + fills)
+            hipLaunchKernelGGL(rank_places_kernel, dim3(blocks + fills), dim3(kSortThreads), 0, stream, tokens, d->index_dtype == FLASHRNN_I64, (uint32_t)n, vocab, keys, places, blocks, fill);
         if (const int e = launch_status()) return e;
         if (n == 0) return FLASHRNN_OK;
     } else {
