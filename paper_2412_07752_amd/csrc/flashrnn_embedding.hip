@@ -25,6 +25,9 @@ constexpr int kColumns = 4;        // columns a lane adds up: neighbours store w
 constexpr uint32_t kMinRun = 8, kMaxRun = 64;   // sorted places that a group of lanes adds up
 constexpr size_t kFillBlocks = 2048, kFillBytes = 8 << 10;   // workgroups that fill, at most; bytes of the table that a wave fills at a time
 constexpr size_t kFillBesideSort = 64 << 20;                  // bytes of the table that are filled beside one launch of a sort of tiles
+// With few places the table is filled beside the ranking, present words or not, but for so many bytes beside the sums, whose words are looked for among the sorted ones: 4096 places of 768 columns
+// among 32000 words 25.4 us, all beside the ranking 26.5; 5000 of 1000 columns among 131072 words 112 and 115, and 132 where all but 64 MB are filled beside the sums.
+constexpr size_t kFillBesideSums = 32 << 20;
 constexpr size_t kFlagsPerBlock = 16 << 10;
 
 __device__ __forceinline__ uint32_t key_of(const void* tokens, bool index64, size_t i, uint32_t vocab) {
@@ -120,11 +123,12 @@ __global__ __launch_bounds__(kThreads) void embedding_fwd_kernel(Lookup q) {
     }
 }
 
-// zeros for rows [begin, end) of the table, `each` (up to 64) at a time a wave: all of them, or those whose flag is not set, neighbours in one go
+// zeros for rows [begin, end) of the table, `each` (up to 64) at a time a wave: all of them, or those whose flag is not set, or whose word is not among n sorted keys; neighbours in one go
 struct Fill {
     float* table;
     const uint8_t* flags;
-    uint32_t begin, end, each;
+    const uint32_t* keys;
+    uint32_t begin, end, each, n;
     int width;
 };
 template <int NT> __device__ __forceinline__ void fill_zeros(const Fill& f, unsigned block, unsigned blocks) {
@@ -135,7 +139,18 @@ template <int NT> __device__ __forceinline__ void fill_zeros(const Fill& f, unsi
     for (uint64_t first = f.begin + ((uint64_t)block * kWaves + threadIdx.x / kWave) * f.each; first < f.end; first += (uint64_t)blocks * kWaves * f.each) {
         const uint64_t row = first + lane;
         const bool in = (uint32_t)lane < f.each && row < f.end;
-        uint64_t absent = __ballot(in && (!f.flags || !f.flags[row]));
+        bool there = false;
+        if (f.flags) {
+            there = in && f.flags[row];
+        } else if (f.keys) {
+            uint32_t lo = 0, hi = in ? f.n : 0;
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (f.keys[mid] < row) lo = mid + 1; else hi = mid;
+            }
+            there = in && lo < f.n && f.keys[lo] == row;
+        }
+        uint64_t absent = __ballot(in && !there);
         while (absent) {
             const int from = __builtin_ctzll(absent);
             const uint64_t rest = ~(absent >> from);
@@ -543,7 +558,7 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
     const Plan p = plan_of(d);
     char* ws = (char*)workspace;
     const size_t row_bytes = (size_t)d->width * 4;
-    Fill fill{(float*)dtable, nullptr, 0, 0, (uint32_t)(row_bytes >= kFillBytes ? 1 : row_bytes * kWave <= kFillBytes ? kWave : kFillBytes / row_bytes), d->width};
+    Fill fill{(float*)dtable, nullptr, nullptr, 0, 0, (uint32_t)(row_bytes >= kFillBytes ? 1 : row_bytes * kWave <= kFillBytes ? kWave : kFillBytes / row_bytes), (uint32_t)n, d->width};
     auto fill_to = [&](uint32_t end, int waves) {   // the rows behind those filled so far; the workgroups for them
         fill.begin = fill.end;
         fill.end = accumulate ? 0 : end;
@@ -551,16 +566,18 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
         return (unsigned)(blocks < kFillBlocks ? blocks : kFillBlocks);
     };
     const uint32_t vocab = (uint32_t)d->vocab;
+    auto fill_beside = [&] { return kFillBesideSort / row_bytes < vocab - fill.end ? fill.end + (uint32_t)(kFillBesideSort / row_bytes) : vocab; };
     uint32_t *keys = (uint32_t*)(ws + p.keys[0]), *places = (uint32_t*)(ws + p.places[0]);
     if (p.tiles == 0) {
-        const unsigned fills = fill_to(vocab, kSortWaves), blocks = (unsigned)((n + kRanked - 1) / kRanked);
+        const uint32_t part = (uint32_t)(kFillBesideSums / row_bytes);
+        const unsigned fills = fill_to(n == 0 || vocab <= part ? vocab : vocab <= 2 * part ? part : vocab - part, kSortWaves), blocks = (unsigned)((n + kRanked - 1) / kRanked);
         if (blocks + fills)
             hipLaunchKernelGGL(rank_places_kernel, dim3(blocks + fills), dim3(kSortThreads), 0, stream, tokens, d->index_dtype == FLASHRNN_I64, (uint32_t)n, vocab, keys, places, blocks, fill);
         if (const int e = launch_status()) return e;
         if (n == 0) return FLASHRNN_OK;
+        fill.keys = keys;
     } else {
         uint8_t* flags = accumulate ? nullptr : (uint8_t*)(ws + p.flags);
-        const size_t rows_at_a_time = kFillBesideSort / row_bytes;
         Pass q{tokens, nullptr, nullptr, nullptr, nullptr, (uint32_t*)(ws + p.counts), flags, (uint32_t)n, p.span, p.tiles, vocab, 0, p.bits, d->index_dtype == FLASHRNN_I64};
         for (int pass = 0; pass < p.passes; ++pass) {
             q.shift = pass * p.bits;
@@ -568,7 +585,7 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
             q.places_out = places = (uint32_t*)(ws + p.places[pass & 1]);
             for (int step = 0; step < 2; ++step) {
                 unsigned more = 0;   // workgroups beside the sort
-                if (pass) more = fill_to(rows_at_a_time < vocab - fill.end ? fill.end + (uint32_t)rows_at_a_time : vocab, kSortWaves);
+                if (pass) more = fill_to(fill_beside(), kSortWaves);
                 else if (step == 0 && flags) more = vocab / kFlagsPerBlock < kFillBlocks ? 1 + vocab / kFlagsPerBlock : kFillBlocks;
                 const dim3 grid(p.tiles + more);
                 if (step == 0) hipLaunchKernelGGL(count_digits_kernel, grid, dim3(kSortThreads), 0, stream, q, fill);
