@@ -429,6 +429,8 @@ def _done(rc, where, result):
 
 
 def _same_device(first, **others):
+    if first.is_cuda and first.device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {first.device}, the current device is cuda:{torch.cuda.current_device()}")
     for name, t in others.items():
         if t is not None and t.device != first.device:
             raise ValueError(f"{name} is on {t.device}, the other tensors on {first.device}")
@@ -443,8 +445,8 @@ def _sized_workspace(workspace, n, device):
     return workspace
 
 
-def flashrnn_embedding_workspace_bytes(tokens, vocab, width=1):
-    """Bytes of workspace of the gradient for this many tokens."""
+def flashrnn_embedding_workspace_bytes(tokens, vocab, width):
+    """Bytes of workspace of the gradient for this many tokens, words and columns."""
     d = flashrnn_embedding_desc_t(int(tokens), int(vocab), int(width), FLASHRNN_F32, FLASHRNN_F32, FLASHRNN_I64, 1.0)
     return lib().flashrnn_embedding_workspace_bytes(ctypes.byref(d))
 
@@ -452,7 +454,10 @@ def flashrnn_embedding_workspace_bytes(tokens, vocab, width=1):
 def flashrnn_embedding_fwd(table, tokens, scale=1.0, dtype=None, out=None, stream=None):
     """out[..., :] = scale * table[tokens[...], :], in the table's type or in `dtype`.  table[vocab, width] bf16 or f32, tokens of any shape, int64 or int32;
     tokens outside the vocabulary give zeros."""
-    if _native is not None and stream is None and out is not None:
+    if stream is not None:   # (what is allocated here belongs to that stream, too)
+        with torch.cuda.stream(stream):
+            return flashrnn_embedding_fwd(table, tokens, scale, dtype, out)
+    if _native is not None and out is not None:
         rc = _native.embedding_fwd(table, tokens, scale, out)
         if rc <= 0:
             return _done(rc, "flashrnn_embedding_fwd", out)
@@ -465,7 +470,7 @@ def flashrnn_embedding_fwd(table, tokens, scale=1.0, dtype=None, out=None, strea
     _chk(out, (*tokens.shape, H), dtype, "out")
     _same_device(table, tokens=tokens, out=out)
     d = flashrnn_embedding_desc_t(tokens.numel(), V, H, _io_dtype(table), _io_dtype(out), _index_dtype(tokens), float(scale))
-    rc = lib().flashrnn_embedding_fwd(ctypes.byref(d), _ptr(table), _ptr(tokens), _ptr(out), _stream(stream))
+    rc = lib().flashrnn_embedding_fwd(ctypes.byref(d), _ptr(table), _ptr(tokens), _ptr(out), _stream(None))
     if rc != FLASHRNN_OK:
         raise FlashRNNError(rc, "flashrnn_embedding_fwd")
     return out
@@ -474,7 +479,10 @@ def flashrnn_embedding_fwd(table, tokens, scale=1.0, dtype=None, out=None, strea
 def flashrnn_embedding_bwd(tokens, dout, vocab, scale=1.0, dtable=None, accumulate=False, workspace=None, stream=None):
     """dtable[v] = scale * sum of dout over the places of word v; dtable[vocab, width] f32.  accumulate: added to the dtable passed in, rows of words that do not
     occur untouched.  The same result on every run."""
-    if _native is not None and stream is None and dtable is not None:
+    if stream is not None:   # (what is allocated here belongs to that stream, too)
+        with torch.cuda.stream(stream):
+            return flashrnn_embedding_bwd(tokens, dout, vocab, scale, dtable, accumulate, workspace)
+    if _native is not None and dtable is not None:
         rc = _native.embedding_bwd(tokens, dout, vocab, scale, dtable, accumulate, workspace)
         if rc <= 0:
             return _done(rc, "flashrnn_embedding_bwd", dtable)
@@ -490,7 +498,7 @@ def flashrnn_embedding_bwd(tokens, dout, vocab, scale=1.0, dtable=None, accumula
     d = flashrnn_embedding_desc_t(tokens.numel(), int(vocab), H, FLASHRNN_F32, _io_dtype(dout), _index_dtype(tokens), float(scale))
     n = lib().flashrnn_embedding_workspace_bytes(ctypes.byref(d))
     workspace = _sized_workspace(workspace, n, dout.device)
-    rc = lib().flashrnn_embedding_bwd(ctypes.byref(d), _ptr(tokens), _ptr(dout), _ptr(dtable), int(bool(accumulate)), _ptr(workspace), _stream(stream))
+    rc = lib().flashrnn_embedding_bwd(ctypes.byref(d), _ptr(tokens), _ptr(dout), _ptr(dtable), int(bool(accumulate)), _ptr(workspace), _stream(None))
     if rc != FLASHRNN_OK:
         raise FlashRNNError(rc, "flashrnn_embedding_bwd")
     return dtable
@@ -538,7 +546,10 @@ def _norm_desc(x, weight, bias, io, dx, eps):
 def flashrnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, dtype=None, save_for_backward=True, y=None, mean=None, rstd=None, stream=None):
     """Layer norm over the last axis of x, in x's type or in `dtype`.  weight, bias: [D], or [NH, D] for x[..., NH, D] (head by head), or None.  x may have one leading
     axis that is not dense, as the hidden states states[1:, 0] of a flashrnn_fwd call.  Returns (y, mean, rstd), the last two f32 of x.shape[:-1], or None, None."""
-    if _native is not None and stream is None and y is not None and (mean is not None and rstd is not None or not save_for_backward):
+    if stream is not None:   # (what is allocated here belongs to that stream, too)
+        with torch.cuda.stream(stream):
+            return flashrnn_layer_norm_fwd(x, weight, bias, eps, dtype, save_for_backward, y, mean, rstd)
+    if _native is not None and y is not None and (mean is not None and rstd is not None or not save_for_backward):
         if not save_for_backward:
             mean = rstd = None
         rc = _native.layer_norm_fwd(x, weight, bias, eps, y, mean, rstd)
@@ -556,7 +567,7 @@ def flashrnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, dtype=None, sav
         mean = rstd = None
     _same_device(x, weight=weight, bias=bias, y=y, mean=mean, rstd=rstd)
     d = _norm_desc(x, weight, bias, y, y, eps)
-    rc = lib().flashrnn_layer_norm_fwd(ctypes.byref(d), _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream))
+    rc = lib().flashrnn_layer_norm_fwd(ctypes.byref(d), _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), _stream(None))
     if rc != FLASHRNN_OK:
         raise FlashRNNError(rc, "flashrnn_layer_norm_fwd")
     return y, mean, rstd
@@ -565,7 +576,10 @@ def flashrnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, dtype=None, sav
 def flashrnn_layer_norm_bwd(dy, x, mean, rstd, weight=None, dtype=None, param_grads=True, out=None, workspace=None, stream=None):
     """Gradient of flashrnn_layer_norm_fwd.  Returns (dx, dweight, dbias): dx dense, in dy's type or in `dtype`; the others f32 in weight's shape ([D] without a weight), or None
     where param_grads is false.  `out` may pass preallocated (dx, dweight, dbias)."""
-    if _native is not None and stream is None and out is not None:
+    if stream is not None:   # (what is allocated here belongs to that stream, too)
+        with torch.cuda.stream(stream):
+            return flashrnn_layer_norm_bwd(dy, x, mean, rstd, weight, dtype, param_grads, out, workspace)
+    if _native is not None and out is not None:
         dx, dweight, dbias = out if param_grads else (out[0], None, None)
         rc = _native.layer_norm_bwd(dy, x, mean, rstd, weight, dx, dweight, dbias, workspace)
         if rc <= 0:
@@ -589,7 +603,7 @@ def flashrnn_layer_norm_bwd(dy, x, mean, rstd, weight=None, dtype=None, param_gr
     if dweight is not None or dbias is not None:
         workspace = _sized_workspace(workspace, lib().flashrnn_layer_norm_workspace_bytes(ctypes.byref(d)), x.device)
     rc = lib().flashrnn_layer_norm_bwd(ctypes.byref(d), _ptr(dy), _ptr(x), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(workspace),
-                                       _stream(stream))
+                                       _stream(None))
     if rc != FLASHRNN_OK:
         raise FlashRNNError(rc, "flashrnn_layer_norm_bwd")
     return dx, dweight, dbias
@@ -609,7 +623,10 @@ def flashrnn_cross_entropy(logits, targets, dloss=None, grad_scale=1.0, gradient
     """Cross entropy of every row of logits[rows, classes] against targets[rows] (int64 or int32; outside the classes: ignored, loss 0), and in the same pass the
     gradient of sum(grad_scale * dloss * loss).  dlogits may be `logits` itself; lse, where passed, takes the rows' log of the sum of exponentials.
     Returns (loss f32[rows], dlogits in logits' type, or None where gradient is false)."""
-    if _native is not None and stream is None and loss is not None and (dlogits is not None or not gradient):
+    if stream is not None:   # (what is allocated here belongs to that stream, too)
+        with torch.cuda.stream(stream):
+            return flashrnn_cross_entropy(logits, targets, dloss, grad_scale, gradient, loss, lse, dlogits)
+    if _native is not None and loss is not None and (dlogits is not None or not gradient):
         if not gradient:
             dlogits = None
         rc = _native.cross_entropy(logits, targets, dloss, grad_scale, loss, lse, dlogits)
@@ -630,7 +647,7 @@ def flashrnn_cross_entropy(logits, targets, dloss=None, grad_scale=1.0, gradient
     to_stride = V if dlogits is None else _matrix(dlogits, (N, V), logits.dtype, "dlogits")
     _same_device(logits, targets=targets, dloss=dloss, loss=loss, lse=lse, dlogits=dlogits)
     d = flashrnn_cross_entropy_desc_t(N, stride, to_stride, V, _io_dtype(logits), _index_dtype(targets), float(grad_scale))
-    rc = lib().flashrnn_cross_entropy(ctypes.byref(d), _ptr(logits), _ptr(targets), _ptr(dloss), _ptr(loss), _ptr(lse), _ptr(dlogits), _stream(stream))
+    rc = lib().flashrnn_cross_entropy(ctypes.byref(d), _ptr(logits), _ptr(targets), _ptr(dloss), _ptr(loss), _ptr(lse), _ptr(dlogits), _stream(None))
     if rc != FLASHRNN_OK:
         raise FlashRNNError(rc, "flashrnn_cross_entropy")
     return loss, dlogits
@@ -639,7 +656,10 @@ def flashrnn_cross_entropy(logits, targets, dloss=None, grad_scale=1.0, gradient
 def flashrnn_grad_clip(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
     """The norm over all values of the tensors in `grads` (bf16 or f32, any mix), and the tensors scaled down so that it is max_norm at most: in place, or into the
     tensors of `out`.  max_norm = inf computes the norm alone (and copies into `out`).  Returns norm f32[1]."""
-    if _native is not None and stream is None and norm is not None:
+    if stream is not None:   # (what is allocated here belongs to that stream, too)
+        with torch.cuda.stream(stream):
+            return flashrnn_grad_clip(grads, max_norm, out, norm, workspace)
+    if _native is not None and norm is not None:
         rc = _native.grad_clip(grads, max_norm, out, norm, workspace, out is not None or max_norm != float("inf"))
         if rc <= 0:
             return _done(rc, "flashrnn_grad_clip", norm)
@@ -657,14 +677,13 @@ def flashrnn_grad_clip(grads, max_norm, out=None, norm=None, workspace=None, str
         _chk(g, g.shape, g.dtype, f"grads[{i}]")
         if o is not g:
             _chk(o, g.shape, g.dtype, f"out[{i}]")
-        if g.device != norm.device or o.device != norm.device:
-            raise ValueError(f"tensor {i} is on {g.device}, norm on {norm.device}")
+        _same_device(norm, grads=g, out=o)
     workspace = _sized_workspace(workspace, lib().flashrnn_grad_clip_workspace_bytes(n), norm.device)
     vp = ctypes.c_void_p * n
     ins = vp(*[g.data_ptr() for g in grads])
     outs = None if out is None and max_norm == float("inf") else vp(*[o.data_ptr() for o in to])
     rc = lib().flashrnn_grad_clip(n, ins, outs, (ctypes.c_longlong * n)(*[g.numel() for g in grads]), (ctypes.c_int * n)(*[_io_dtype(g) for g in grads]), float(max_norm),
-                                  _ptr(norm), _ptr(workspace), _stream(stream))
+                                  _ptr(norm), _ptr(workspace), _stream(None))
     if rc != FLASHRNN_OK:
         raise FlashRNNError(rc, "flashrnn_grad_clip")
     return norm

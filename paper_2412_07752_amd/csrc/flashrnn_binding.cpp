@@ -147,13 +147,13 @@ int small(int64_t v) {
     need(v >= 0 && v < INT32_MAX);
     return (int)v;
 }
-// the tensors of a call: all on one device
+// the tensors of a call: all on the current device
 struct Operands {
+    const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream();
     const at::Tensor* first = nullptr;
     const at::Tensor* take(const at::Tensor* t) {
-        need(t != nullptr);
+        need(t != nullptr && t->device().index() == stream.device_index());
         if (!first) first = t;
-        need(t->device() == first->device());
         return t;
     }
     const at::Tensor* dense(PyObject* o) { return take(plain(o)); }
@@ -171,7 +171,6 @@ struct Operands {
     }
 };
 void* pointer(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
-void* current_stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
 // f() with everything it throws turned into a call handed back (nothing throws behind the library's call)
 template <typename F> PyObject* answer(F&& f) {
@@ -198,7 +197,7 @@ PyObject* embedding_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         need(table->dim() == 2 && out->dim() == tokens->dim() + 1 && out->sizes().slice(0, tokens->dim()) == tokens->sizes() && out->size(-1) == table->size(1));
         const flashrnn_embedding_desc_t d{tokens->numel(), small(table->size(0)), small(table->size(1)), io_type(table->scalar_type()), io_type(out->scalar_type()),
                                           index_type(tokens->scalar_type()), number(a[2])};
-        void *tp = pointer(table), *ip = pointer(tokens), *op = pointer(out), *stream = current_stream();
+        void *tp = pointer(table), *ip = pointer(tokens), *op = pointer(out), *stream = ops.stream.stream();
         return without_lock([&] { return p_embedding_fwd(&d, tp, ip, op, stream); });
     });
 }
@@ -217,7 +216,7 @@ PyObject* embedding_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* dtable = ops.dense(a[4], at::kFloat, {(int64_t)small(vocab), H});
         const flashrnn_embedding_desc_t d{tokens->numel(), (int)vocab, small(H), FLASHRNN_F32, io_type(dout->scalar_type()), index_type(tokens->scalar_type()), number(a[3])};
         const at::Tensor ws = ops.workspace(a[6], p_embedding_bytes(&d));
-        void *ip = pointer(tokens), *dp = pointer(dout), *tp = pointer(dtable), *wp = pointer(&ws), *stream = current_stream();
+        void *ip = pointer(tokens), *dp = pointer(dout), *tp = pointer(dtable), *wp = pointer(&ws), *stream = ops.stream.stream();
         const int accumulate = a[5] == Py_True;
         return without_lock([&] { return p_embedding_bwd(&d, ip, dp, tp, accumulate, wp, stream); });
     });
@@ -265,7 +264,7 @@ PyObject* layer_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::IntArrayRef lead = x->sizes().slice(0, x->dim() - 1);
         const at::Tensor *mean = ops.optional(a[5], at::kFloat, lead), *rstd = ops.optional(a[6], at::kFloat, lead);
         const auto d = norm_desc(x, weight ? weight : bias, y->scalar_type(), y->scalar_type(), number(a[3]));
-        void *xp = pointer(x), *wp = pointer(weight), *bp = pointer(bias), *yp = pointer(y), *mp = pointer(mean), *rp = pointer(rstd), *stream = current_stream();
+        void *xp = pointer(x), *wp = pointer(weight), *bp = pointer(bias), *yp = pointer(y), *mp = pointer(mean), *rp = pointer(rstd), *stream = ops.stream.stream();
         return without_lock([&] { return p_norm_fwd(&d, xp, wp, bp, yp, mp, rp, stream); });
     });
 }
@@ -284,7 +283,7 @@ PyObject* layer_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor ws;
         if (dweight || dbias) ws = ops.workspace(a[8], p_norm_bytes(&d));
         void *gp = pointer(dy), *xp = pointer(x), *wp = pointer(weight), *mp = pointer(mean), *rp = pointer(rstd), *dp = pointer(dx), *dwp = pointer(dweight), *dbp = pointer(dbias);
-        void *sp = ws.defined() ? pointer(&ws) : nullptr, *stream = current_stream();
+        void *sp = ws.defined() ? pointer(&ws) : nullptr, *stream = ops.stream.stream();
         return without_lock([&] { return p_norm_bwd(&d, gp, xp, wp, mp, rp, dp, dwp, dbp, sp, stream); });
     });
 }
@@ -307,7 +306,7 @@ PyObject* cross_entropy(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor *dloss = ops.optional(a[2], at::kFloat, {N}), *loss = ops.dense(a[4], at::kFloat, {N}), *lse = ops.optional(a[5], at::kFloat, {N});
         const flashrnn_cross_entropy_desc_t d{N, row_stride(logits), dlogits ? row_stride(dlogits) : V, small(V), io_type(logits->scalar_type()), index_type(targets->scalar_type()),
                                               number(a[3])};
-        void *xp = pointer(logits), *tp = pointer(targets), *gp = pointer(dloss), *lp = pointer(loss), *sp = pointer(lse), *dp = pointer(dlogits), *stream = current_stream();
+        void *xp = pointer(logits), *tp = pointer(targets), *gp = pointer(dloss), *lp = pointer(loss), *sp = pointer(lse), *dp = pointer(dlogits), *stream = ops.stream.stream();
         return without_lock([&] { return p_cross_entropy(&d, xp, tp, gp, lp, sp, dp, stream); });
     });
 }
@@ -333,7 +332,7 @@ PyObject* grad_clip(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         const float max_norm = number(a[1]);
         const at::Tensor ws = ops.workspace(a[4], p_clip_bytes((int)count));
-        void *wp = pointer(&ws), *stream = current_stream();
+        void *wp = pointer(&ws), *stream = ops.stream.stream();
         void* const* to = a[5] == Py_True ? out.data() : nullptr;
         return without_lock([&] { return p_grad_clip((int)count, in.data(), to, sizes.data(), types.data(), max_norm, norm, wp, stream); });
     });

@@ -556,6 +556,7 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
     if (!aligned_to(dout, type_size(d->io_dtype)) || !aligned_to(tokens, type_size(d->index_dtype)) || !aligned_to(dtable, 4)) return FLASHRNN_ERR_UNSUPPORTED;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const Plan p = plan_of(d);
+    if ((double)p.runs * p.column_blocks * p.L >= 4e9) return FLASHRNN_ERR_UNSUPPORTED;   // (more than any memory holds)
     char* ws = (char*)workspace;
     const size_t row_bytes = (size_t)d->width * 4;
     Fill fill{(float*)dtable, nullptr, nullptr, 0, 0, (uint32_t)(row_bytes >= kFillBytes ? 1 : row_bytes * kWave <= kFillBytes ? kWave : kFillBytes / row_bytes), (uint32_t)n, d->width};

@@ -545,6 +545,26 @@ def test_operators_run_on_the_current_stream_and_on_the_one_passed():
     assert torch.equal(out, want[0])
 
 
+def test_what_a_call_on_another_stream_allocates_belongs_to_that_stream():
+    """Behind a wait on the stream passed, while the current stream takes and fills all memory that the allocator hands out again."""
+    s = _buffers(1)
+    want = [t.clone() for t in _all_of_them(s)]
+    stream = torch.cuda.Stream()
+    for _ in range(3):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(10_000_000)
+        x = api.flashrnn_embedding_fwd(s["table"], s["tokens"], stream=stream)
+        y, mean, rstd = api.flashrnn_layer_norm_fwd(x, s["weight"], s["bias"], stream=stream)
+        loss, dy = api.flashrnn_cross_entropy(y, s["tokens"], stream=stream)
+        dx, dweight, dbias = api.flashrnn_layer_norm_bwd(dy, x, mean, rstd, s["weight"], stream=stream)
+        dtable = api.flashrnn_embedding_bwd(s["tokens"], dx, len(s["table"]), stream=stream)
+        norm = api.flashrnn_grad_clip([dtable, dweight, dbias], 0.1, stream=stream)
+        junk = [torch.full((1 << k,), 123, dtype=torch.uint8, device="cuda") for k in range(9, 23)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((x, y, loss, dy, dx, dweight, dbias, dtable, norm), want)), len(junk)
+
+
 def test_operators_in_a_graph():
     """Captured once and replayed on new inputs, with eager work between the replays."""
     s = _buffers(2)
