@@ -22,7 +22,8 @@ constexpr int kTileRounds = 2;     // places per thread of a tile at a time
 constexpr int kRows = 4;           // places that a group of lanes looks up at a time, where there are kManyWaves waves of places
 constexpr uint64_t kManyWaves = 16384;
 constexpr int kColumns = 4;        // columns a lane adds up: neighbours store whole cache lines of float32 (with eight, each store left every second 16 bytes out)
-constexpr uint32_t kMinRun = 8, kMaxRun = 64;   // sorted places that a group of lanes adds up
+// Sorted places that a group of lanes adds up.  Up to kOneRun places are one run: no pieces, a launch less (32 places of 64 columns 9.5 us and 11.8, but 64 of 768 columns 14.7 and 12.0).
+constexpr uint32_t kMinRun = 8, kMaxRun = 64, kOneRun = 32;
 constexpr size_t kFillBlocks = 2048, kFillBytes = 8 << 10;   // workgroups that fill, at most; bytes of the table that a wave fills at a time
 constexpr size_t kFillBesideSort = 64 << 20;                  // bytes of the table that are filled beside one launch of a sort of tiles
 // With few places the table is filled beside the ranking, present words or not, but for so many bytes beside the sums, whose words are looked for among the sorted ones: 4096 places of 768 columns
@@ -492,7 +493,7 @@ Plan plan_of(const flashrnn_embedding_desc_t* d) {
     // places per run: enough runs for 2048 waves, as long as that leaves them kMinRun places or more
     const size_t waves = n * p.column_blocks * p.L / kWave;
     p.run = kMaxRun;
-    while (p.run > kMinRun && waves / p.run < 2048) p.run /= 2;
+    while (n > kOneRun && p.run > kMinRun && waves / p.run < 2048) p.run /= 2;
     p.runs = (uint32_t)((n + p.run - 1) / p.run);
     size_t at = 0;
     const size_t list = up(n * 4);
