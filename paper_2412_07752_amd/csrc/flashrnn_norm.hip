@@ -1,12 +1,17 @@
 // Layer norm over the rows of a tensor, one weight row for all of them or one per head, and its gradient (include/flashrnn.h).
+//
+// y = (x - mean) rstd w + b;  dx = rstd (g - E g - xh E(g xh)) with g = dy w, xh = (x - mean) rstd;  dw = sum dy xh, db = sum dy.  Both directions are bound by memory: x (and dy) are read once, y (or dx)
+// is written once, and the row stays in registers between its sums; the mean first, then the squares around it, so that an offset costs no digits.  All sums are float32.  Measured:
+// forward 65536 x 8 x 256 float32 states to bf16 141 us (5.7 TB/s), 65536 x 2048 bf16 91 us (5.9 TB/s); gradient 65536 x 8 x 256 197 us (5.5 TB/s), 16384 x 768 bf16 18.6 us (4.1 TB/s, 4 us of it the
+// second kernel).  Rows of fewer than 8 values, and of more than 8192 (forward in bf16 and gradients all in bf16: 16384), take general kernels that read them several times (10000 float32 values: 1.5 TB/s forward, 1.0 backward).
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;
 
 namespace {
 
-// Workgroups of a forward call: 65536 x 8 x 256 states take 161 us with 768 workgroups of 256 threads, 162 with 2048, 148 with 8192 and 160 with one row for every
-// group of threads.
+// Workgroups of a forward call: 65536 x 8 x 256 states (stored through the caches) take 161 us with 768 workgroups of 256 threads, 162 with 2048, 148 with 8192 and 160 with one row for
+// every group of threads.
 constexpr unsigned kMostThreads = 8192 * 256;
 // ... and of a gradient, whose workgroups each leave partial sums of dweight and dbias: 16384 x 768 values in bf16 take 20.2 us with 256 workgroups of 256 threads, 18.6 with 512, 19.2 with 768
 // and 20.0 with 1024; 65536 x 8 x 256 states 191, 197, 213 and 220, 65536 x 1200 in bf16 153, 100, 97 and 98.
