@@ -247,7 +247,7 @@ typedef enum { FLASHRNN_I32 = 2, FLASHRNN_I64 = 3 } flashrnn_index_t;
  */
 typedef struct {
     long long tokens;   /* >= 0, below 2^29 for the gradient */
-    int vocab, width;   /* > 0; width at most 2^23 */
+    int vocab, width;   /* > 0; width at most 2^20 */
     int table_dtype, io_dtype, index_dtype;
     float scale;
 } flashrnn_embedding_desc_t;

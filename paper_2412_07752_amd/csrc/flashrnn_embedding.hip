@@ -400,17 +400,17 @@ __global__ __launch_bounds__(kThreads) void sum_runs_kernel(Sum q, Fill fill) {
     put_row<ACCUMULATE>(q, col, word, word == before ? pieces : word == after ? pieces + q.width : nullptr, s);
 }
 
-// A workgroup per run (and 256 columns): where a word begins in the run and goes on beyond it, its pieces are added up, every kJoinWaves-th by a wave, and its row is written.
-constexpr int kJoinWaves = 4;
-template <bool NARROW>
-__global__ __launch_bounds__(kJoinWaves * kWave) void join_pieces_kernel(Sum q, uint32_t runs) {
-    constexpr int V = 4, kAhead = 4;
-    __shared__ float lds[kJoinWaves][kWave][V];
+// A workgroup per run (and L * kColumns columns): where a word begins in the run and goes on beyond it, its pieces are added up, every kGroups-th by a group of L lanes, and its row is written.
+template <int L, bool NARROW>
+__global__ __launch_bounds__(kThreads) void join_pieces_kernel(Sum q, uint32_t runs) {
+    constexpr int V = kColumns, kGroups = kThreads / L, kAhead = 8;
+    __shared__ float lds[kGroups][L][V];
     const uint32_t r = blockIdx.x, b = r * q.run, e = q.n - b < q.run ? q.n : b + q.run;
     if (e == q.n) return;
     const uint32_t word = q.keys[e - 1];
     if (word == q.vocab || q.keys[e] != word || (b && q.keys[b - 1] == word)) return;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, l = threadIdx.x % L;
+    const uint32_t group = threadIdx.x / L;
     uint32_t more = 0;   // runs that the word goes on through: those that begin with it
     while (true) {
         const uint64_t next = (uint64_t)r + 1 + more + lane;
@@ -421,35 +421,33 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void join_pieces_kernel(Sum q, 
         }
         more += kWave;
     }
-    const Columns<V, NARROW> col(blockIdx.y * kWave + lane, q.width);
+    const Columns<V, NARROW> col(blockIdx.y * L + l, q.width);
     const size_t step = 2 * (size_t)q.width;
     const float* from = q.pieces + (size_t)r * step;
     float s[V] = {};
-    if (w == 0) {
+    if (group == 0) {
         const Chunk<float, V> c = col.load(from + q.width);
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = c.get(i);
     }
-    for (uint32_t k = 1 + w; k <= more; k += kAhead * kJoinWaves) {
+    for (uint32_t k = 1 + group; k <= more; k += kAhead * kGroups) {
         Chunk<float, V> c[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const uint32_t at = k + u * kJoinWaves <= more ? k + u * kJoinWaves : more;
-            c[u] = col.load(from + at * step);
-        }
+        for (int u = 0; u < kAhead; ++u) c[u] = col.load(from + (k + u * kGroups <= more ? k + u * kGroups : more) * step);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (k + u * kJoinWaves <= more)
+            if (k + u * kGroups <= more)
 #pragma unroll
                 for (int i = 0; i < V; ++i) s[i] += c[u].get(i);
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) lds[w][lane][i] = s[i];
+    for (int i = 0; i < V; ++i) lds[group][l][i] = s[i];
     __syncthreads();
-    if (w) return;
-    for (int v = 1; v < kJoinWaves; ++v)
+    if (group) return;
+    const int groups = more + 1 < kGroups ? (int)more + 1 : kGroups;   // (that have added anything)
+    for (int v = 1; v < groups; ++v)
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[i] += lds[v][lane][i];
+        for (int i = 0; i < V; ++i) s[i] += lds[v][l][i];
     if (q.accumulate) put_row<true>(q, col, word, nullptr, s);
     else put_row<false>(q, col, word, nullptr, s);
 }
@@ -459,7 +457,7 @@ int check_desc(const flashrnn_embedding_desc_t* d, bool gradient) {
     if (d->tokens < 0 || d->vocab <= 0 || d->width <= 0) return FLASHRNN_ERR_SHAPE;
     if (!is_io_type(d->table_dtype) || !is_io_type(d->io_dtype) || !is_index_type(d->index_dtype)) return FLASHRNN_ERR_SHAPE;
     // every offset below 2^62 bytes; the gradient's workgroups (one per run of places, and so on) below 2^32 threads, 2^16 in the other direction
-    if ((double)d->tokens * d->width > 1e18 || d->width > (1 << 23) || (gradient && d->tokens >= (1LL << 29))) return FLASHRNN_ERR_UNSUPPORTED;
+    if ((double)d->tokens * d->width > 1e18 || d->width > (1 << 20) || (gradient && d->tokens >= (1LL << 29))) return FLASHRNN_ERR_UNSUPPORTED;
     return FLASHRNN_OK;
 }
 
@@ -608,25 +606,26 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
     const unsigned fill_blocks = fill_to(vocab, kThreads / kWave);   // (with few places: none are left)
     const uint32_t sum_blocks = (uint32_t)(((size_t)p.runs * p.column_blocks + kThreads / p.L - 1) / (kThreads / p.L));
     const Sum q{keys, places, dout, (float*)dtable, (float*)(ws + p.pieces), (uint32_t)n, vocab, p.run, d->width, accumulate, d->scale, (uint32_t)p.column_blocks, sum_blocks};
-    const int e = with_io_type(d->io_dtype, [&](auto* ot) {
-        using O = std::remove_pointer_t<decltype(ot)>;
-        const dim3 grid(sum_blocks + fill_blocks);
-        auto launch = [&](auto lanes, auto narrow) {
-            if (accumulate) hipLaunchKernelGGL((sum_runs_kernel<O, decltype(lanes)::value, decltype(narrow)::value, true>), grid, dim3(kThreads), 0, stream, q, fill);
-            else hipLaunchKernelGGL((sum_runs_kernel<O, decltype(lanes)::value, decltype(narrow)::value, false>), grid, dim3(kThreads), 0, stream, q, fill);
-        };
+    auto by_lanes = [&](auto&& launch) {
         if (d->width < kColumns) launch(Int<8>{}, Int<1>{});
         else if (p.L == 64) launch(Int<64>{}, Int<0>{});
         else if (p.L == 32) launch(Int<32>{}, Int<0>{});
         else if (p.L == 16) launch(Int<16>{}, Int<0>{});
         else launch(Int<8>{}, Int<0>{});
         return launch_status();
+    };
+    const int e = with_io_type(d->io_dtype, [&](auto* ot) {
+        using O = std::remove_pointer_t<decltype(ot)>;
+        const dim3 grid(sum_blocks + fill_blocks);
+        return by_lanes([&](auto lanes, auto narrow) {
+            if (accumulate) hipLaunchKernelGGL((sum_runs_kernel<O, decltype(lanes)::value, decltype(narrow)::value, true>), grid, dim3(kThreads), 0, stream, q, fill);
+            else hipLaunchKernelGGL((sum_runs_kernel<O, decltype(lanes)::value, decltype(narrow)::value, false>), grid, dim3(kThreads), 0, stream, q, fill);
+        });
     });
     if (e != FLASHRNN_OK || p.runs == 1) return e;
-    const dim3 grid(p.runs, (d->width + 4 * kWave - 1) / (4 * kWave));
-    if (d->width < 4) hipLaunchKernelGGL((join_pieces_kernel<true>), grid, dim3(kJoinWaves * kWave), 0, stream, q, p.runs);
-    else hipLaunchKernelGGL((join_pieces_kernel<false>), grid, dim3(kJoinWaves * kWave), 0, stream, q, p.runs);
-    return launch_status();
+    return by_lanes([&](auto lanes, auto narrow) {
+        hipLaunchKernelGGL((join_pieces_kernel<decltype(lanes)::value, decltype(narrow)::value>), dim3(p.runs, p.column_blocks), dim3(kThreads), 0, stream, q, p.runs);
+    });
 }
 
 }  // extern "C"

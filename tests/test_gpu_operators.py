@@ -91,6 +91,31 @@ def test_embedding_gradient_of_very_frequent_words(n, vocab, width, words, dtype
     assert torch.equal(got, api.flashrnn_embedding_bwd(tokens, dout, vocab))
 
 
+@pytest.mark.parametrize("n,vocab,width", [(300, 300_000, 8), (12288, 262_143, 24), (12289, 262_143, 24), (12000, 262_144, 24), (20_000, 2_000_000, 4), (300_001, 70_000, 16), (600_000, 513, 12)])
+@pytest.mark.parametrize("index", [torch.int64, torch.int32])
+def test_embedding_gradient_of_every_way_to_sort(n, vocab, width, index):
+    """Few and many places, words of one to three digits, tiles of several steps; with padding on both sides of the vocabulary."""
+    gen = _gen(n)
+    tokens, dout = _tokens(gen, n, vocab, index), _normal(gen, n, width)
+    want, bound = ou.embedding_grad(tokens, dout, vocab, 0.5)
+    got = api.flashrnn_embedding_bwd(tokens, dout, vocab, scale=0.5)
+    ou.check(got, want, bound, "dtable")
+    assert torch.equal(got, api.flashrnn_embedding_bwd(tokens, dout, vocab, scale=0.5))
+    again = api.flashrnn_embedding_bwd(tokens, dout, vocab, scale=0.5, dtable=got.clone(), accumulate=True)
+    ou.check(again, 2 * want, 2 * bound + 2 * ou.U * want.abs(), "accumulated")
+
+
+def test_embedding_of_places_beyond_32_bit_offsets():
+    n, width = (1 << 31) // 4096 + 5000, 4096
+    tokens = torch.zeros(n, dtype=torch.int32, device="cuda")
+    tokens[-3:] = torch.tensor([7, 5, 7], dtype=torch.int32)
+    table = torch.arange(9, device="cuda", dtype=BF16)[:, None].expand(9, width).contiguous()
+    out = api.flashrnn_embedding_fwd(table, tokens)
+    assert out[-3:].float().mean(1).tolist() == [7.0, 5.0, 7.0] and not out[:-3].any()
+    dtable = api.flashrnn_embedding_bwd(tokens, out, 9)
+    assert (dtable[7] == 14).all() and (dtable[5] == 5).all() and not dtable[[0, 1, 2, 3, 4, 6, 8]].any()
+
+
 def test_embedding_of_no_tokens_and_of_padding_alone():
     table = torch.randn(9, 12, device="cuda")
     none = torch.empty((0, 4), dtype=torch.int64, device="cuda")
