@@ -3,7 +3,8 @@
 // y = (x - mean) rstd w + b;  dx = rstd (g - E g - xh E(g xh)) with g = dy w, xh = (x - mean) rstd;  dw = sum dy xh, db = sum dy.  Both directions are bound by memory: x (and dy) are read once, y (or dx)
 // is written once, and the row stays in registers between its sums; the mean first, then the squares around it, so that an offset costs no digits.  All sums are float32.  Measured:
 // forward 65536 x 8 x 256 float32 states to bf16 141 us (5.7 TB/s), 65536 x 2048 bf16 91 us (5.9 TB/s); gradient 65536 x 8 x 256 197 us (5.5 TB/s), 16384 x 768 bf16 18.6 us (4.1 TB/s, 4 us of it the
-// second kernel).  Rows of fewer than 8 values, and of more than 8192 (forward in bf16 and gradients all in bf16: 16384), take general kernels that read them several times (10000 float32 values: 1.5 TB/s forward, 1.0 backward).
+// second kernel).  Rows of fewer than 8 values, and of more than 16384 (bf16: 24576) forward or 12288 (all bf16: 16384) backward, take general kernels that read them several times (30000 float32 values: 1.1 TB/s
+// forward; 16000: 1.2 backward).
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;
@@ -409,10 +410,13 @@ template <typename F> void with_grad_shape(const flashrnn_layer_norm_desc_t* d, 
     with_io_type(d->x_dtype, [&](auto* xt) {
         return with_io_type(d->io_dtype, [&](auto* yt) {
             if (with_shape<true>((d->width + 3) / 4, [&](auto s) { f(xt, yt, Int<4>{}, s); })) return 0;
-            if constexpr (sizeof(*xt) == 2 && sizeof(*yt) == 2) {   // rows of more than 8192 values
+            // rows of more than 8192 values
+            if constexpr (sizeof(*xt) == 2 && sizeof(*yt) == 2) {
                 const int chunks = (d->width + 7) / 8;
                 if (chunks <= 512 * 3) f(xt, yt, Int<8>{}, Shape<512, 3>{});
                 else if (chunks <= 512 * 4) f(xt, yt, Int<8>{}, Shape<512, 4>{});
+            } else {
+                if (d->width <= 1024 * 3 * 4) f(xt, yt, Int<4>{}, Shape<1024, 3>{});
             }
             return 0;
         });
@@ -449,7 +453,8 @@ int flashrnn_layer_norm_fwd(const flashrnn_layer_norm_desc_t* d, const void* x, 
     if (d->width >= 8) with_io_type(d->x_dtype, [&](auto* xt) {
         using X = std::remove_pointer_t<decltype(xt)>;
         constexpr int V = 16 / sizeof(X);
-        return (int)with_shape<true>((d->width + V - 1) / V, [&](auto s) {
+        const int chunks = (d->width + V - 1) / V;
+        auto launch = [&](auto s) {
             constexpr int L = decltype(s)::L, K = decltype(s)::K, NT = threads_of<L>();
             const unsigned blocks = blocks_for(rows, NT / L, d->groups, kMostThreads / NT);
             if (!blocks) return;
@@ -457,7 +462,12 @@ int flashrnn_layer_norm_fwd(const flashrnn_layer_norm_desc_t* d, const void* x, 
             hipLaunchKernelGGL((layer_norm_rows_kernel<X, V, L, K>), dim3(blocks), dim3(NT), 0, (hipStream_t)hip_stream, r, (const X*)x, weight, bias,
                                d->param_dtype == FLASHRNN_BF16, y, d->io_dtype == FLASHRNN_BF16, rows * d->width * type_size(d->io_dtype) > kStreamBytes, (float*)mean, (float*)rstd, d->eps);
             status = launch_status();
-        });
+        };
+        if (!with_shape<true>(chunks, launch)) {   // rows that a workgroup of 1024 threads holds
+            if (chunks <= 1024 * 3) launch(Shape<1024, 3>{});
+            else if (V == 4 && chunks <= 1024 * 4) launch(Shape<1024, V == 4 ? 4 : 3>{});
+        }
+        return 0;
     });
     if (taken) return status;
     return with_io_type(d->x_dtype, [&](auto* xt) {
