@@ -1,7 +1,7 @@
 // Embedding lookup and its gradient by sorted tokens (include/flashrnn.h).
 //
 // out_i = s E[tok_i];  dE[v] = s sum over the places i of v of dout_i, every sum in float32 and in the order of the places, so that no result hangs on which workgroup comes first.  Both are bound by
-// memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 162 us (4.2 TB/s: a sort of four launches takes 29 us of it, the sums
+// memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 160 us (4.2 TB/s: a sort of four launches takes 27 us of it, the sums
 // and the zeros beside them 125, the pieces 9), 4096 places x 768 columns into 32000 words 25.4 us.
 //
 // The gradient sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs, beyond by a radix sort, least significant digit
@@ -240,7 +240,8 @@ __global__ __launch_bounds__(kSortThreads) void rank_places_kernel(const void* _
     places_out[rank] = i;
 }
 
-// One pass over more places (two launches of 5 and 9 us at 65536 places; counting the next digit in the same launch, with atomics, takes 29 us: half the words of a text share it): workgroup `tile` of `tiles` takes `span` of them.  keys == nullptr: the first digit, straight from the tokens.
+// One pass over more places (two launches of 5 and 8 us at 65536 places; counting the next digit in the same launch, with atomics, takes 29 us: half the words of a text share it): workgroup `tile` of `tiles`
+// takes `span` of them.  FIRST: the first digit, straight from the tokens.
 struct Pass {
     const void* tokens;
     const uint32_t *keys, *places;
@@ -249,12 +250,12 @@ struct Pass {
     uint32_t n, span, tiles, vocab;
     int shift, bits, index64;
 };
-__device__ __forceinline__ uint32_t key_at(const Pass& p, uint32_t i) { return p.keys ? p.keys[i] : key_of(p.tokens, p.index64, i, p.vocab); }
+template <bool FIRST> __device__ __forceinline__ uint32_t key_at(const Pass& p, uint32_t i) { return FIRST ? key_of(p.tokens, p.index64, i, p.vocab) : p.keys[i]; }
 
-__global__ __launch_bounds__(kSortThreads) void count_digits_kernel(Pass p, Fill fill) {
+template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void count_digits_kernel(Pass p, Fill fill) {
     __shared__ uint32_t lds[kDigits];
     if (blockIdx.x >= p.tiles) {
-        if (p.flags && !p.keys)
+        if (FIRST && p.flags)
             for (uint64_t i = (uint64_t)(blockIdx.x - p.tiles) * kSortThreads + threadIdx.x; i <= p.vocab; i += (uint64_t)(gridDim.x - p.tiles) * kSortThreads) p.flags[i] = 0;
         return fill_zeros<kSortThreads>(fill, blockIdx.x - p.tiles, gridDim.x - p.tiles);
     }
@@ -262,60 +263,84 @@ __global__ __launch_bounds__(kSortThreads) void count_digits_kernel(Pass p, Fill
     if (threadIdx.x < kDigits) lds[threadIdx.x] = 0;
     __syncthreads();
     const uint64_t begin = (uint64_t)blockIdx.x * p.span, end = begin + p.span < p.n ? begin + p.span : p.n;
-    for (uint64_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&lds[key_at(p, (uint32_t)i) >> p.shift & mask], 1u);   // (whole numbers: any order)
+    for (uint64_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&lds[key_at<FIRST>(p, (uint32_t)i) >> p.shift & mask], 1u);   // (whole numbers: any order)
     __syncthreads();
     if (threadIdx.x < kDigits) p.counts[(size_t)blockIdx.x * kDigits + threadIdx.x] = lds[threadIdx.x];
 }
 
-__global__ __launch_bounds__(kSortThreads) void move_places_kernel(Pass p, Fill fill) {
-    __shared__ uint32_t counts[kSortWaves][kDigits], next[kDigits], totals[kDigits / kWave];
+template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void move_places_kernel(Pass p, Fill fill) {
+    __shared__ uint32_t counts[kSortWaves][kDigits], all[kSortThreads], before_me[kSortThreads], totals[kDigits / kWave];
     if (blockIdx.x >= p.tiles) return fill_zeros<kSortThreads>(fill, blockIdx.x - p.tiles, gridDim.x - p.tiles);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const uint32_t mask = (1u << p.bits) - 1;
-    // where this tile's places of each digit go: behind all smaller digits, and the same one in the tiles before
-    uint32_t total = 0, mine = 0;
-    if (threadIdx.x < kDigits)
-        for (uint32_t t = 0; t < p.tiles; t += 8) {   // (eight loads on their way)
-            uint32_t c[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) c[u] = p.counts[(size_t)(t + u < p.tiles ? t + u : p.tiles - 1) * kDigits + threadIdx.x];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                mine += t + u < blockIdx.x ? c[u] : 0;
-                total += t + u < p.tiles ? c[u] : 0;
-            }
-        }
-    const uint32_t before = scan_digits(total, totals);
-    if (threadIdx.x < kDigits) next[threadIdx.x] = before + mine;
+    const int wide = p.bits < 6 ? 6 : p.bits;   // (a digit has at most 16 threads in the sums of the counts)
+    const uint32_t mask = (1u << p.bits) - 1, digits = 1u << wide;
     const uint64_t begin = (uint64_t)blockIdx.x * p.span, end = begin + p.span < p.n ? begin + p.span : p.n;
-    for (uint64_t at = begin; at < end; at += kSortThreads * kTileRounds) {
-        for (int d = threadIdx.x; d < kSortWaves * kDigits; d += kSortThreads) counts[0][d] = 0;
-        __syncthreads();
-        uint32_t key[kTileRounds], rank[kTileRounds], place[kTileRounds];
+    uint32_t key[kTileRounds], rank[kTileRounds], place[kTileRounds];
+    // (No branch around a load: lanes beyond the tile read its last place.  With `in ? ... : ...` around them the compiler has been seen to drop the copy of a place whose register the token had taken.)
+    auto fetch = [&](uint64_t at) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kTileRounds; ++u) {
             const uint64_t i = at + (w * kTileRounds + u) * kWave + lane;
-            const bool in = i < end;
-            key[u] = in ? key_at(p, (uint32_t)i) : ~0u;
-            place[u] = in && p.places ? p.places[i] : (uint32_t)i;
+            place[u] = (uint32_t)(i < end ? i : end - 1);
+            key[u] = key_at<FIRST>(p, place[u]);
         }
+#pragma unroll
+        for (int u = 0; u < kTileRounds; ++u) {
+            if (!FIRST) place[u] = p.places[place[u]];
+            if (at + (w * kTileRounds + u) * kWave + lane >= end) key[u] = ~0u;
+        }
+    };
+    fetch(begin);
+    // where this tile's places of each digit go: behind all smaller digits, and the same one in the tiles before.  The threads of a digit share the tiles, with eight loads on their way
+    {
+        const uint32_t parts = kSortThreads >> wide, each = (p.tiles + parts - 1) / parts, first = (threadIdx.x >> wide) * each, digit = threadIdx.x & (digits - 1);
+        uint32_t total = 0, mine = 0;
+        for (uint32_t t = 0; t < each; t += 8) {
+            uint32_t c[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) c[u] = p.counts[(size_t)(first + t + u < p.tiles ? first + t + u : p.tiles - 1) * kDigits + digit];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const uint32_t tile = first + t + u, count = t + u < each && tile < p.tiles ? c[u] : 0;
+                mine += tile < blockIdx.x ? count : 0;
+                total += count;
+            }
+        }
+        all[threadIdx.x] = total;
+        before_me[threadIdx.x] = mine;
+    }
+    __syncthreads();
+    uint32_t total = 0, next = 0;
+    if (threadIdx.x < digits)
+        for (uint32_t part = threadIdx.x; part < kSortThreads; part += digits) {
+            total += all[part];
+            next += before_me[part];
+        }
+    next += scan_digits(total, totals);   // (of the thread's digit)
+    for (uint64_t at = begin; at < end; at += kSortThreads * kTileRounds) {
+        if (at != begin) fetch(at);
+        if (threadIdx.x <= mask)
+#pragma unroll
+            for (int v = 0; v < kSortWaves; ++v) counts[v][threadIdx.x] = 0;
+        __syncthreads();
 #pragma unroll
         for (int u = 0; u < kTileRounds; ++u) rank[u] = rank_in_wave(key[u] >> p.shift & mask, key[u] != ~0u, p.bits, counts[w]);
         __syncthreads();
-        if (threadIdx.x < kDigits) {
-            uint32_t to = next[threadIdx.x];
+        if (threadIdx.x <= mask) {
+            uint32_t c[kSortWaves];
+#pragma unroll
+            for (int v = 0; v < kSortWaves; ++v) c[v] = counts[v][threadIdx.x];
+#pragma unroll
             for (int v = 0; v < kSortWaves; ++v) {
-                const uint32_t c = counts[v][threadIdx.x];
-                counts[v][threadIdx.x] = to;
-                to += c;
+                counts[v][threadIdx.x] = next;
+                next += c[v];
             }
-            next[threadIdx.x] = to;
         }
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < kTileRounds; ++u)
             if (key[u] != ~0u) {
-                if (p.flags && !p.keys) p.flags[key[u]] = 1;
+                if (FIRST && p.flags) p.flags[key[u]] = 1;
                 const uint32_t to = counts[w][key[u] >> p.shift & mask] + rank[u];
                 p.keys_out[to] = key[u];
                 p.places_out[to] = place[u];
@@ -594,8 +619,8 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
                 if (pass) more = fill_to(fill_beside(), kSortWaves);
                 else if (step == 0 && flags) more = vocab / kFlagsPerBlock < kFillBlocks ? 1 + vocab / kFlagsPerBlock : kFillBlocks;
                 const dim3 grid(p.tiles + more);
-                if (step == 0) hipLaunchKernelGGL(count_digits_kernel, grid, dim3(kSortThreads), 0, stream, q, fill);
-                else hipLaunchKernelGGL(move_places_kernel, grid, dim3(kSortThreads), 0, stream, q, fill);
+                if (step == 0) hipLaunchKernelGGL((pass ? count_digits_kernel<false> : count_digits_kernel<true>), grid, dim3(kSortThreads), 0, stream, q, fill);
+                else hipLaunchKernelGGL((pass ? move_places_kernel<false> : move_places_kernel<true>), grid, dim3(kSortThreads), 0, stream, q, fill);
                 if (const int e = launch_status()) return e;
                 fill.flags = flags;
             }
