@@ -1,7 +1,7 @@
 // Embedding lookup and its gradient by sorted tokens (include/flashrnn.h).
 //
 // out_i = s E[tok_i];  dE[v] = s sum over the places i of v of dout_i, every sum in float32 and in the order of the places, so that no result hangs on which workgroup comes first.  Both are bound by
-// memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 160 us (4.2 TB/s: a sort of four launches takes 27 us of it, the sums
+// memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 159 us (4.3 TB/s: a sort of four launches takes 27 us of it, the sums
 // and the zeros beside them 125, the pieces 9), 4096 places x 768 columns into 32000 words 25.4 us.
 //
 // The gradient sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs, beyond by a radix sort, least significant digit
@@ -425,56 +425,88 @@ __global__ __launch_bounds__(kThreads) void sum_runs_kernel(Sum q, Fill fill) {
     put_row<ACCUMULATE>(q, col, word, word == before ? pieces : word == after ? pieces + q.width : nullptr, s);
 }
 
-// A workgroup per run (and L * kColumns columns): where a word begins in the run and goes on beyond it, its pieces are added up, every kGroups-th by a group of L lanes, and its row is written.
+// Where a word begins in a run and goes on beyond it, its pieces are added up in order and its row is written.  Most such words go on through one or two runs: a group of L lanes per run (and L * kColumns
+// columns) adds them up, behind the first `longs` workgroups.  These have one window of kManyRuns runs each, in which at most one word can begin that goes on through kManyRuns or more: the whole
+// workgroup looks for its end and adds it up, its groups every kGroups-th piece.  (A workgroup for every run instead: 18750 runs of 64 columns take 2 us more,
+// 31250 of 64 columns, with words of thousands of runs, 6 us.)
+constexpr int kManyRuns = 8;
 template <int L, bool NARROW>
-__global__ __launch_bounds__(kThreads) void join_pieces_kernel(Sum q, uint32_t runs) {
-    constexpr int V = kColumns, kGroups = kThreads / L, kAhead = 8;
+__global__ __launch_bounds__(kThreads) void join_pieces_kernel(Sum q, uint32_t runs, uint32_t longs) {
+    constexpr int V = kColumns, kGroups = kThreads / L;
     __shared__ float lds[kGroups][L][V];
-    const uint32_t r = blockIdx.x, b = r * q.run, e = q.n - b < q.run ? q.n : b + q.run;
-    if (e == q.n) return;
-    const uint32_t word = q.keys[e - 1];
-    if (word == q.vocab || q.keys[e] != word || (b && q.keys[b - 1] == word)) return;
     const int lane = threadIdx.x & 63, l = threadIdx.x % L;
     const uint32_t group = threadIdx.x / L;
-    uint32_t more = 0;   // runs that the word goes on through: those that begin with it
-    while (true) {
-        const uint64_t next = (uint64_t)r + 1 + more + lane;
-        const uint64_t m = __ballot(next < runs && q.keys[next < runs ? next * q.run : 0] == word);
-        if (~m) {
-            more += __builtin_ctzll(~m);
-            break;
-        }
-        more += kWave;
-    }
+    const bool is_long = blockIdx.x < longs;
     const Columns<V, NARROW> col(blockIdx.y * L + l, q.width);
     const size_t step = 2 * (size_t)q.width;
-    const float* from = q.pieces + (size_t)r * step;
-    float s[V] = {};
-    if (group == 0) {
+    // s += pieces k, k + by, ... up to `last` of those at `from`, AHEAD of them on their way
+    auto add = [&](auto ahead, float(&s)[V], const float* from, uint32_t k, uint32_t by, uint32_t last) __attribute__((always_inline)) {
+        constexpr int kAhead = decltype(ahead)::value;
+        for (; k <= last; k += kAhead * by) {
+            Chunk<float, V> c[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) c[u] = col.load(from + (k + u * by <= last ? k + u * by : last) * step);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (k + u * by <= last)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) s[i] += c[u].get(i);
+        }
+    };
+    auto begin = [&](float(&s)[V], const float* from) __attribute__((always_inline)) {   // the piece in the run itself
         const Chunk<float, V> c = col.load(from + q.width);
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = c.get(i);
+    };
+    auto put = [&](uint32_t word, float(&s)[V]) __attribute__((always_inline)) {
+        if (q.accumulate) put_row<true>(q, col, word, nullptr, s);
+        else put_row<false>(q, col, word, nullptr, s);
+    };
+    // the word that run r ends with, if it begins there and goes on, or else vocab
+    auto word_from = [&](uint32_t r) __attribute__((always_inline)) {
+        if (r + 1 >= runs) return q.vocab;
+        const uint32_t b = r * q.run, e = b + q.run, before = q.keys[b ? b - 1 : 0], word = q.keys[e - 1];
+        return q.keys[e] == word && !(b && before == word) ? word : q.vocab;
+    };
+    auto begins_with = [&](uint32_t r, uint32_t word) __attribute__((always_inline)) { return r < runs && q.keys[r < runs ? (size_t)r * q.run : 0] == word; };
+    if (!is_long) {
+        const uint32_t r = (blockIdx.x - longs) * kGroups + group, word = word_from(r);
+        // runs that it goes on through: those that begin with it, of the next kManyRuns
+        const uint64_t m = __ballot(word != q.vocab && l < kManyRuns && begins_with(r + 1 + l, word)) >> (lane - l);
+        const int more = __builtin_ctzll(~(m & ((1ull << kManyRuns) - 1)));
+        if (more == 0 || more == kManyRuns) return;
+        const float* from = q.pieces + (size_t)r * step;
+        float s[V];
+        begin(s, from);
+        add(Int<4>{}, s, from, 1, 1, more);
+        put(word, s);
+        return;
     }
-    for (uint32_t k = 1 + group; k <= more; k += kAhead * kGroups) {
-        Chunk<float, V> c[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) c[u] = col.load(from + (k + u * kGroups <= more ? k + u * kGroups : more) * step);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (k + u * kGroups <= more)
-#pragma unroll
-                for (int i = 0; i < V; ++i) s[i] += c[u].get(i);
+    const uint32_t first = blockIdx.x * kManyRuns + lane % kManyRuns, mine = word_from(first);
+    const uint64_t there = __ballot(mine != q.vocab && begins_with(first + kManyRuns, mine));
+    if (!there) return;
+    const uint32_t r = blockIdx.x * kManyRuns + __builtin_ctzll(there), word = q.keys[(size_t)(r + 1) * q.run];
+    uint32_t lo = r + 1 + kManyRuns, hi = runs;   // run lo - 1 begins with the word, run hi does not, or is none: 64 between them are looked at at a time
+    while (lo < hi) {
+        const uint32_t part = (hi - lo + kWave - 1) / kWave;
+        const uint32_t n = __popcll(__ballot(lo + lane * part < hi && begins_with(lo + lane * part, word))), to = lo + n * part;
+        hi = n == 0 ? lo : to < hi ? to : hi;
+        lo = n == 0 ? lo : lo + (n - 1) * part + 1;
     }
+    const uint32_t more = lo - 1 - r;
+    const float* from = q.pieces + (size_t)r * step;
+    float s[V] = {};
+    if (group == 0) begin(s, from);
+    add(Int<8>{}, s, from, 1 + group, kGroups, more);
 #pragma unroll
     for (int i = 0; i < V; ++i) lds[group][l][i] = s[i];
     __syncthreads();
     if (group) return;
-    const int groups = more + 1 < kGroups ? (int)more + 1 : kGroups;   // (that have added anything)
-    for (int v = 1; v < groups; ++v)
+    const uint32_t groups = more + 1 < (uint32_t)kGroups ? more + 1 : kGroups;   // (that have added anything)
+    for (uint32_t v = 1; v < groups; ++v)
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] += lds[v][l][i];
-    if (q.accumulate) put_row<true>(q, col, word, nullptr, s);
-    else put_row<false>(q, col, word, nullptr, s);
+    put(word, s);
 }
 
 int check_desc(const flashrnn_embedding_desc_t* d, bool gradient) {
@@ -649,7 +681,9 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
     });
     if (e != FLASHRNN_OK || p.runs == 1) return e;
     return by_lanes([&](auto lanes, auto narrow) {
-        hipLaunchKernelGGL((join_pieces_kernel<decltype(lanes)::value, decltype(narrow)::value>), dim3(p.runs, p.column_blocks), dim3(kThreads), 0, stream, q, p.runs);
+        constexpr unsigned kGroups = kThreads / decltype(lanes)::value;
+        const unsigned longs = (p.runs + kManyRuns - 1) / kManyRuns;
+        hipLaunchKernelGGL((join_pieces_kernel<decltype(lanes)::value, decltype(narrow)::value>), dim3(longs + (p.runs + kGroups - 1) / kGroups, p.column_blocks), dim3(kThreads), 0, stream, q, p.runs, longs);
     });
 }
 
