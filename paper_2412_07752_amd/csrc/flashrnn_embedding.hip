@@ -19,7 +19,8 @@ constexpr int kDigits = 1 << kDigitBits;
 // Places that are sorted by counting, the bits of their numbers, and those that a workgroup ranks.  Whole gradients of 80 columns: 11525 places 24.3 us by counting and 31.7 by tiles,
 // 16000 places 34.2 and 27.0.
 constexpr int kSmall = 12288, kSmallBits = 14, kRanked = 16;
-constexpr int kMaxTiles = 128;     // tiles of a larger sort
+// Tiles of a larger sort, each of which adds up the counts of all: 300000 places of 64 columns 49.5 us, with 128 tiles 53.9 and with 512 as with 256; a million 66.3, 68.8, and with 512 90.
+constexpr int kMaxTiles = 256;
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / kWave;
 constexpr int kTileRounds = 2;     // places per thread of a tile at a time
