@@ -1,11 +1,11 @@
 // Embedding lookup and its gradient by sorted tokens (include/flashrnn.h).
 //
 // out_i = s E[tok_i];  dE[v] = s sum over the places i of v of dout_i, every sum in float32 and in the order of the places, so that no result hangs on which workgroup comes first.  Both are bound by
-// memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 159 us (4.3 TB/s: a sort of four launches takes 27 us of it, the sums
-// and the zeros beside them 125, the pieces 9), 4096 places x 768 columns into 32000 words 25.4 us.
+// memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 158 us (4.3 TB/s: a sort of four launches takes 27 us of it, the sums
+// and the zeros beside them 123, the pieces 8), 4096 places x 768 columns into 32000 words 25.9 us, 32 places of 64 columns 4.9 us.
 //
-// The gradient sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs, beyond by a radix sort, least significant digit
-// first, of tiles of places.  The table's rows are filled with zeros by the workgroups that the sort leaves idle.  Then groups of lanes
+// The gradient of up to kFewPlaces places is one launch.  Beyond, it sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs,
+// beyond by a radix sort, least significant digit first, of tiles of places.  The table's rows are filled with zeros by the workgroups that the sort leaves idle.  Then groups of lanes
 // add up runs of consecutive sorted places and write the rows of the words that begin and end inside; what is left of a word at the ends of a run goes to the workspace, and a last kernel joins such pieces
 // in order.  Tokens outside the vocabulary sort behind all words.
 #include "flashrnn_rows.h"
@@ -27,14 +27,13 @@ constexpr int kTileRounds = 2;     // places per thread of a tile at a time
 constexpr int kRows = 4;           // places that a group of lanes looks up at a time, where there are kManyWaves waves of places
 constexpr uint64_t kManyWaves = 16384;
 constexpr int kColumns = 4;        // columns a lane adds up: neighbours store whole cache lines of float32 (with eight, each store left every second 16 bytes out)
-// Sorted places that a group of lanes adds up.  Up to kOneRun places are one run: no pieces, a launch less (32 places of 64 columns 9.5 us and 11.8, but 64 of 768 columns 14.7 and 12.0).
-constexpr uint32_t kMinRun = 8, kMaxRun = 64, kOneRun = 32;
-constexpr size_t kFillBlocks = 2048, kFillBytes = 8 << 10;   // workgroups that fill, at most; bytes of the table that a wave fills at a time
+constexpr uint32_t kMinRun = 8, kMaxRun = 64;   // sorted places that a group of lanes adds up
+constexpr size_t kFillWaves = 32768, kFillBytes = 8 << 10;   // waves that fill, at most; bytes of the table that a wave fills at a time
 constexpr size_t kFillBesideSort = 64 << 20;                  // bytes of the table that are filled beside one launch of a sort of tiles
 // With few places the table is filled beside the ranking, present words or not, but for so many bytes beside the sums, whose words are looked for among the sorted ones: 4096 places of 768 columns
 // among 32000 words 25.4 us, all beside the ranking 26.5; 5000 of 1000 columns among 131072 words 112 and 115, and 132 where all but 64 MB are filled beside the sums.
 constexpr size_t kFillBesideSums = 32 << 20;
-constexpr size_t kFlagsPerBlock = 16 << 10;
+constexpr size_t kFlagsPerBlock = 16 << 10, kFlagBlocks = 2048;
 
 __device__ __forceinline__ uint32_t key_of(const void* tokens, bool index64, size_t i, uint32_t vocab) {
     const int64_t t = index64 ? ((const int64_t*)tokens)[i] : ((const int32_t*)tokens)[i];
@@ -130,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void embedding_fwd_kernel(Lookup q) {
     }
 }
 
-// zeros for rows [begin, end) of the table, `each` (up to 64) at a time a wave: all of them, or those whose flag is not set, or whose word is not among n sorted keys; neighbours in one go
+// zeros for rows [begin, end) of the table, `each` (up to 64) at a time a wave, but for those that are `there`; neighbours in one go
 struct Fill {
     float* table;
     const uint8_t* flags;
@@ -138,26 +137,16 @@ struct Fill {
     uint32_t begin, end, each, n;
     int width;
 };
-template <int NT> __device__ __forceinline__ void fill_zeros(const Fill& f, unsigned block, unsigned blocks) {
+// there(first, row, in): whether the lane's row, one of those from `first` on, is left alone (in: it is one of [begin, end))
+template <int NT, typename There> __device__ __forceinline__ void fill_rows(const Fill& f, unsigned block, unsigned blocks, There there) {
     constexpr int kWaves = NT / kWave;
     const int lane = threadIdx.x & 63;
     Chunk<float, 4> zero;
     zero.clear();
     for (uint64_t first = f.begin + ((uint64_t)block * kWaves + threadIdx.x / kWave) * f.each; first < f.end; first += (uint64_t)blocks * kWaves * f.each) {
         const uint64_t row = first + lane;
-        const bool in = (uint32_t)lane < f.each && row < f.end;
-        bool there = false;
-        if (f.flags) {
-            there = in && f.flags[row];
-        } else if (f.keys) {
-            uint32_t lo = 0, hi = in ? f.n : 0;
-            while (lo < hi) {
-                const uint32_t mid = (lo + hi) / 2;
-                if (f.keys[mid] < row) lo = mid + 1; else hi = mid;
-            }
-            there = in && lo < f.n && f.keys[lo] == row;
-        }
-        uint64_t absent = __ballot(in && !there);
+        const bool in = (uint32_t)lane < f.each && row < f.end, stays = there((uint32_t)first, row, in);   // (by all lanes)
+        uint64_t absent = __ballot(in && !stays);
         while (absent) {
             const int from = __builtin_ctzll(absent);
             const uint64_t rest = ~(absent >> from);
@@ -173,6 +162,19 @@ template <int NT> __device__ __forceinline__ void fill_zeros(const Fill& f, unsi
             absent &= ~0ull << (from + count);
         }
     }
+}
+// all rows, or those whose flag is not set, or whose word is not among n sorted keys
+template <int NT> __device__ __forceinline__ void fill_zeros(const Fill& f, unsigned block, unsigned blocks) {
+    fill_rows<NT>(f, block, blocks, [&](uint32_t, uint64_t row, bool in) __attribute__((always_inline)) {
+        if (f.flags) return in && f.flags[row];
+        if (!f.keys) return false;
+        uint32_t lo = 0, hi = in ? f.n : 0;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (f.keys[mid] < row) lo = mid + 1; else hi = mid;
+        }
+        return in && lo < f.n && f.keys[lo] == row;
+    });
 }
 
 // Digits of 64 places a wave at a time: lanes with the same digit find each other by comparing the digits' bits; a lane's rank is the number of lower lanes with its
@@ -510,6 +512,91 @@ __global__ __launch_bounds__(kThreads) void join_pieces_kernel(Sum q, uint32_t r
     put(word, s);
 }
 
+// Up to kFewPlaces places, one launch: a workgroup per place (and one of `spread` parts of the column blocks) looks for the places of its word and, where none comes before its own, adds them up: each
+// group of L lanes a part of them, in order, and the parts in order.  The workgroups beyond fill, with the words in their registers.  Every workgroup reads all tokens, so there are up to kFewBlocks
+// of them, with up to two column blocks each, and no more columns than that: 32 places of 64 columns 4.9 us, by sorting 9.0; 1024 of 768 columns among 300 words 8.1 and 11.7; 512 of 4096 columns
+// 8.9 and 11.6 (without the limit 1024 of 4096 columns 16.5 and 13.8).
+constexpr uint32_t kFewPlaces = 1024, kFewBlocks = 4096;
+template <typename O, int L, bool NARROW, bool ACCUMULATE>
+__global__ __launch_bounds__(kThreads) void few_places_kernel(Sum q, const void* tokens, bool index64, uint32_t spread, Fill fill) {
+    constexpr int V = kColumns, kGroups = kThreads / L, kAhead = 8, kWaves = kThreads / kWave, kParts = kFewPlaces / kWave;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (blockIdx.x >= q.blocks) {
+        __shared__ uint32_t words[kWaves][2];
+        uint32_t keys[kParts];   // (no row's number: none)
+#pragma unroll
+        for (int u = 0; u < kParts; ++u) {
+            const uint32_t i = u * kWave + lane, key = i < q.n ? key_of(tokens, index64, i, q.vocab) : q.vocab;
+            keys[u] = key < q.vocab ? key : ~0u;
+        }
+        return fill_rows<kThreads>(fill, blockIdx.x - q.blocks, gridDim.x - q.blocks, [&](uint32_t first, uint64_t, bool) __attribute__((always_inline)) {
+            bool any = false;
+#pragma unroll
+            for (int u = 0; u < kParts; ++u) any |= keys[u] - first < fill.each;
+            if (!__ballot(any)) return false;
+            if (lane < 2) words[w][lane] = 0;   // (one wave: its LDS accesses are in order)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (int u = 0; u < kParts; ++u)
+                if (keys[u] - first < fill.each) atomicOr(&words[w][(keys[u] - first) / 32], 1u << (keys[u] - first) % 32);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const bool there = words[w][lane / 32] >> lane % 32 & 1;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            return there;
+        });
+    }
+    __shared__ uint64_t masks[kParts];
+    __shared__ uint32_t places[kFewPlaces];
+    __shared__ float lds[kGroups][L][V];
+    const uint32_t own = blockIdx.x / spread, word = key_of(tokens, index64, own, q.vocab);
+    if (word == q.vocab) return;
+    uint64_t mask[kParts / kWaves];   // places of the word, 64 at a time; the wave's
+#pragma unroll
+    for (int u = 0; u < kParts / kWaves; ++u) {
+        const uint32_t i = u * kThreads + threadIdx.x;
+        mask[u] = __ballot(key_of(tokens, index64, i < q.n ? i : q.n - 1, q.vocab) == word && i < q.n);
+        if (lane == 0) masks[u * kWaves + w] = mask[u];
+    }
+    __syncthreads();
+    uint32_t total = 0, earlier = 0;   // places of the word: all, before the workgroup's own
+#pragma unroll
+    for (int v = 0; v < kParts; ++v) {
+        const uint64_t m = masks[v];
+        if (v == (int)(own / kWave)) earlier = total + __popcll(m & ((1ull << own % kWave) - 1));
+        if (v % kWaves == w && mask[v / kWaves] >> lane & 1) places[total + __popcll(m & ((1ull << lane) - 1))] = v * kWave + lane;
+        total += __popcll(m);
+    }
+    if (earlier) return;
+    __syncthreads();
+    const int l = threadIdx.x % L;
+    const uint32_t group = threadIdx.x / L, part = (total + kGroups - 1) / kGroups, end = (group + 1) * part < total ? (group + 1) * part : total;
+    for (uint32_t block = blockIdx.x - own * spread; block < q.column_blocks; block += spread) {
+        const Columns<V, NARROW> col(block * L + l, q.width);
+        float s[V] = {};
+        for (uint32_t k = group * part; k < end; k += kAhead) {
+            Chunk<O, V> rows[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) rows[u] = col.load((const O*)q.dout + (size_t)places[k + u < end ? k + u : end - 1] * q.width);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (k + u < end)
+#pragma unroll
+                    for (int c = 0; c < V; ++c) s[c] += rows[u].get(c);
+        }
+        if (total > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < V; ++c) lds[group][l][c] = s[c];
+            __syncthreads();
+        }
+        if (group) continue;
+        for (uint32_t v = 1; v * part < total; ++v)
+#pragma unroll
+            for (int c = 0; c < V; ++c) s[c] += lds[v][l][c];
+        put_row<ACCUMULATE>(q, col, word, nullptr, s);
+    }
+}
+
 int check_desc(const flashrnn_embedding_desc_t* d, bool gradient) {
     if (!d) return FLASHRNN_ERR_NULL;
     if (d->tokens < 0 || d->vocab <= 0 || d->width <= 0) return FLASHRNN_ERR_SHAPE;
@@ -555,7 +642,7 @@ Plan plan_of(const flashrnn_embedding_desc_t* d) {
     // places per run: enough runs for 2048 waves, as long as that leaves them kMinRun places or more
     const size_t waves = n * p.column_blocks * p.L / kWave;
     p.run = kMaxRun;
-    while (n > kOneRun && p.run > kMinRun && waves / p.run < 2048) p.run /= 2;
+    while (p.run > kMinRun && waves / p.run < 2048) p.run /= 2;
     p.runs = (uint32_t)((n + p.run - 1) / p.run);
     size_t at = 0;
     const size_t list = up(n * 4);
@@ -627,18 +714,36 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
         fill.begin = fill.end;
         fill.end = accumulate ? 0 : end;
         const size_t parts = ((size_t)fill.end - fill.begin + fill.each - 1) / fill.each, blocks = (parts + waves - 1) / waves;
-        return (unsigned)(blocks < kFillBlocks ? blocks : kFillBlocks);
+        return (unsigned)(blocks < kFillWaves / waves ? blocks : kFillWaves / waves);
     };
     const uint32_t vocab = (uint32_t)d->vocab;
+    auto by_lanes = [&](auto&& launch) {
+        if (d->width < kColumns) launch(Int<8>{}, Int<1>{});
+        else if (p.L == 64) launch(Int<64>{}, Int<0>{});
+        else if (p.L == 32) launch(Int<32>{}, Int<0>{});
+        else if (p.L == 16) launch(Int<16>{}, Int<0>{});
+        else launch(Int<8>{}, Int<0>{});
+        return launch_status();
+    };
+    if (n <= kFewPlaces && n * p.column_blocks <= 2 * kFewBlocks) {
+        const unsigned fills = fill_to(vocab, kThreads / kWave), each = n * p.column_blocks > kFewBlocks ? 2 : 1, spread = (p.column_blocks + each - 1) / each, blocks = (unsigned)n * spread;
+        if (blocks + fills == 0) return FLASHRNN_OK;
+        const Sum q{nullptr, nullptr, dout, (float*)dtable, nullptr, (uint32_t)n, vocab, 0, d->width, accumulate, d->scale, (uint32_t)p.column_blocks, blocks};
+        return with_io_type(d->io_dtype, [&](auto* ot) {
+            using O = std::remove_pointer_t<decltype(ot)>;
+            return by_lanes([&](auto lanes, auto narrow) {
+                auto kernel = accumulate ? few_places_kernel<O, decltype(lanes)::value, decltype(narrow)::value, true> : few_places_kernel<O, decltype(lanes)::value, decltype(narrow)::value, false>;
+                hipLaunchKernelGGL(kernel, dim3(blocks + fills), dim3(kThreads), 0, stream, q, tokens, d->index_dtype == FLASHRNN_I64, spread, fill);
+            });
+        });
+    }
     auto fill_beside = [&] { return kFillBesideSort / row_bytes < vocab - fill.end ? fill.end + (uint32_t)(kFillBesideSort / row_bytes) : vocab; };
     uint32_t *keys = (uint32_t*)(ws + p.keys[0]), *places = (uint32_t*)(ws + p.places[0]);
     if (p.tiles == 0) {
         const uint32_t part = (uint32_t)(kFillBesideSums / row_bytes);
-        const unsigned fills = fill_to(n == 0 || vocab <= part ? vocab : vocab <= 2 * part ? part : vocab - part, kSortWaves), blocks = (unsigned)((n + kRanked - 1) / kRanked);
-        if (blocks + fills)
-            hipLaunchKernelGGL(rank_places_kernel, dim3(blocks + fills), dim3(kSortThreads), 0, stream, tokens, d->index_dtype == FLASHRNN_I64, (uint32_t)n, vocab, keys, places, blocks, fill);
+        const unsigned fills = fill_to(vocab <= part ? vocab : vocab <= 2 * part ? part : vocab - part, kSortWaves), blocks = (unsigned)((n + kRanked - 1) / kRanked);
+        hipLaunchKernelGGL(rank_places_kernel, dim3(blocks + fills), dim3(kSortThreads), 0, stream, tokens, d->index_dtype == FLASHRNN_I64, (uint32_t)n, vocab, keys, places, blocks, fill);
         if (const int e = launch_status()) return e;
-        if (n == 0) return FLASHRNN_OK;
         fill.keys = keys;
     } else {
         uint8_t* flags = accumulate ? nullptr : (uint8_t*)(ws + p.flags);
@@ -650,7 +755,7 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
             for (int step = 0; step < 2; ++step) {
                 unsigned more = 0;   // workgroups beside the sort
                 if (pass) more = fill_to(fill_beside(), kSortWaves);
-                else if (step == 0 && flags) more = vocab / kFlagsPerBlock < kFillBlocks ? 1 + vocab / kFlagsPerBlock : kFillBlocks;
+                else if (step == 0 && flags) more = vocab / kFlagsPerBlock < kFlagBlocks ? 1 + vocab / kFlagsPerBlock : kFlagBlocks;
                 const dim3 grid(p.tiles + more);
                 if (step == 0) hipLaunchKernelGGL((pass ? count_digits_kernel<false> : count_digits_kernel<true>), grid, dim3(kSortThreads), 0, stream, q, fill);
                 else hipLaunchKernelGGL((pass ? move_places_kernel<false> : move_places_kernel<true>), grid, dim3(kSortThreads), 0, stream, q, fill);
@@ -664,14 +769,6 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
     const unsigned fill_blocks = fill_to(vocab, kThreads / kWave);   // (with few places: none are left)
     const uint32_t sum_blocks = (uint32_t)(((size_t)p.runs * p.column_blocks + kThreads / p.L - 1) / (kThreads / p.L));
     const Sum q{keys, places, dout, (float*)dtable, (float*)(ws + p.pieces), (uint32_t)n, vocab, p.run, d->width, accumulate, d->scale, (uint32_t)p.column_blocks, sum_blocks};
-    auto by_lanes = [&](auto&& launch) {
-        if (d->width < kColumns) launch(Int<8>{}, Int<1>{});
-        else if (p.L == 64) launch(Int<64>{}, Int<0>{});
-        else if (p.L == 32) launch(Int<32>{}, Int<0>{});
-        else if (p.L == 16) launch(Int<16>{}, Int<0>{});
-        else launch(Int<8>{}, Int<0>{});
-        return launch_status();
-    };
     const int e = with_io_type(d->io_dtype, [&](auto* ot) {
         using O = std::remove_pointer_t<decltype(ot)>;
         const dim3 grid(sum_blocks + fill_blocks);
@@ -680,7 +777,7 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
             else hipLaunchKernelGGL((sum_runs_kernel<O, decltype(lanes)::value, decltype(narrow)::value, false>), grid, dim3(kThreads), 0, stream, q, fill);
         });
     });
-    if (e != FLASHRNN_OK || p.runs == 1) return e;
+    if (e != FLASHRNN_OK) return e;
     return by_lanes([&](auto lanes, auto narrow) {
         constexpr unsigned kGroups = kThreads / decltype(lanes)::value;
         const unsigned longs = (p.runs + kManyRuns - 1) / kManyRuns;

@@ -105,6 +105,22 @@ def test_embedding_gradient_of_every_way_to_sort(n, vocab, width, index):
     ou.check(again, 2 * want, 2 * bound + 2 * ou.U * want.abs(), "accumulated")
 
 
+@pytest.mark.parametrize("n,vocab,width", [(1, 1, 1), (64, 65, 3), (65, 64, 2), (1024, 300, 40), (1025, 300, 40), (1023, 100_000, 7), (1024, 2000, 1100), (900, 7, 2048), (1024, 40, 2050), (3, 5, 70_000)])
+@pytest.mark.parametrize("dtype,index", [(F32, torch.int32), (BF16, torch.int64)])
+def test_embedding_gradient_of_few_places(n, vocab, width, dtype, index):
+    """Around the largest number of places, and of places times columns, that one launch takes; words all different, all the same, and in between."""
+    gen = _gen(n + width)
+    words = _tokens(gen, n, vocab, index)
+    dout = _normal(gen, n, width, dtype=dtype)
+    for tokens in (words, torch.full_like(words, vocab - 1), torch.arange(n, dtype=index, device="cuda") * 2 - 1):
+        want, bound = ou.embedding_grad(tokens, dout, vocab, 1.5)
+        got = api.flashrnn_embedding_bwd(tokens, dout, vocab, scale=1.5, dtable=torch.full((vocab, width), float("nan"), device="cuda"))
+        ou.check(got, want, bound, "dtable")
+        assert torch.equal(got, api.flashrnn_embedding_bwd(tokens, dout, vocab, scale=1.5))
+        again = api.flashrnn_embedding_bwd(tokens, dout, vocab, scale=1.5, dtable=got.clone(), accumulate=True)
+        ou.check(again, 2 * want, 2 * bound + 2 * ou.U * want.abs(), "accumulated")
+
+
 def test_embedding_of_places_beyond_32_bit_offsets():
     n, width = (1 << 31) // 4096 + 5000, 4096
     tokens = torch.zeros(n, dtype=torch.int32, device="cuda")
