@@ -2,8 +2,8 @@
 //
 // y = (x - mean) rstd w + b;  dx = rstd (g - E g - xh E(g xh)) with g = dy w, xh = (x - mean) rstd;  dw = sum dy xh, db = sum dy.  Both directions are bound by memory: x (and dy) are read once, y (or dx)
 // is written once, and the row stays in registers between its sums; the mean first, then the squares around it, so that an offset costs no digits.  All sums are float32.  Measured:
-// forward 65536 x 8 x 256 float32 states to bf16 141 us (5.7 TB/s), 65536 x 2048 bf16 91 us (5.9 TB/s); gradient 65536 x 8 x 256 197 us (5.5 TB/s), 16384 x 768 bf16 18.6 us (4.1 TB/s, 4 us of it the
-// second kernel).  Rows of fewer than 8 values, and of more than 16384 (bf16: 24576) forward or 12288 (all bf16: 16384) backward, take general kernels that read them several times (30000 float32 values: 1.1 TB/s
+// forward 65536 x 8 x 256 float32 states to bf16 141 us (5.7 TB/s), 65536 x 2048 bf16 91 us (5.9 TB/s); gradient 65536 x 8 x 256 197 us (5.5 TB/s), 16384 x 768 bf16 18.7 us (4.0 TB/s, 4 us of it the
+// second kernel), up to 512 rows in one launch: 64 x 768 bf16 5.4 us.  Rows of fewer than 8 values, and of more than 16384 (bf16: 24576) forward or 12288 (all bf16: 16384) backward, take general kernels that read them several times (30000 float32 values: 1.1 TB/s
 // forward; 16000: 1.2 backward).
 #include "flashrnn_rows.h"
 
@@ -129,16 +129,72 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_rows_kernel(Rows r
 // The gradient, rows in registers as above: dx from the row's two sums, and every thread's part of dweight and dbias in its registers over all rows that its group takes.
 // At the end the groups of a workgroup that share a row of the weights meet in LDS and their sum, in the order of the groups, is one row of partial sums; with more
 // rows of weights than groups every group writes its own.  dweight, dbias: [strips][groups][width] each, a strip for every workgroup, or for every `groups` groups of threads; or null.
-template <typename X, typename Y, int V, int L, int K>
-__global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(Rows r, const Y* __restrict__ dy, const X* __restrict__ x, const void* __restrict__ weight,
+// COLUMNS, for few rows: every group of threads takes one row, for dx alone, and the first `column_blocks` workgroups add up dweight and dbias themselves, each kSumColumns columns over all rows.
+constexpr int kSumColumns = 32;
+template <typename X, typename Y, int NT>
+__device__ __forceinline__ void sum_columns(const Rows& r, const Y* __restrict__ dy, const X* __restrict__ x, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
+                                            float* __restrict__ dweight, float* __restrict__ dbias) {
+    constexpr int V = 4, L = kSumColumns / V, kGroups = NT / L, kAhead = 4;
+    __shared__ float lds[NT / kWave][L][2 * V];
+    const int l = threadIdx.x % L, blocks = (r.width + kSumColumns - 1) / kSumColumns, g = blockIdx.x / blocks, from = (blockIdx.x - g * blocks) * kSumColumns + l * V;
+    const int at = from < r.width - V ? from : r.width - V;   // (of columns that two lanes have, both write the same sums)
+    const uint32_t tokens = r.count / r.groups;
+    float s[2 * V] = {};
+    for (uint32_t t = threadIdx.x / L; t < tokens; t += kAhead * kGroups) {
+        Chunk<X, V> raw_x[kAhead];
+        Chunk<Y, V> raw_dy[kAhead];
+        float mean[kAhead], rstd[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t row = (t + u * kGroups < tokens ? t + u * kGroups : tokens - 1) * r.groups + g;
+            raw_x[u].load(x + x_offset(r, row) + at);
+            raw_dy[u].load(dy + (size_t)row * r.width + at);
+            mean[u] = mean_in[row];
+            rstd[u] = rstd_in[row];
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (t + u * kGroups < tokens)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    s[i] += raw_dy[u].get(i) * ((raw_x[u].get(i) - mean[u]) * rstd[u]);
+                    s[V + i] += raw_dy[u].get(i);
+                }
+    }
+#pragma unroll
+    for (int o = L; o < kWave; o *= 2)
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) s[i] += __shfl_xor(s[i], o);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (lane < L)
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) lds[w][l][i] = s[i];
+    __syncthreads();
+    if (threadIdx.x >= L) return;
+#pragma unroll
+    for (int v = 1; v < NT / kWave; ++v)
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) s[i] += lds[v][l][i];
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float* out = which ? dbias : dweight;
+        if (!out) continue;
+        Chunk<float, V> c;
+#pragma unroll
+        for (int i = 0; i < V; ++i) c.w[i] = __builtin_bit_cast(uint32_t, s[which * V + i]);
+        c.store(out + (size_t)g * r.width + at);
+    }
+}
+template <typename X, typename Y, int V, int L, int K, bool COLUMNS>
+__global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(uint32_t column_blocks, Rows r, const Y* __restrict__ dy, const X* __restrict__ x, const void* __restrict__ weight,
                                                                               bool weight_bf16, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
                                                                               void* __restrict__ dx, bool dx_bf16, bool stream, float* __restrict__ dweight, float* __restrict__ dbias) {
     constexpr int NT = threads_of<L>(), PER = NT / L;
+    if (COLUMNS && blockIdx.x < column_blocks) return sum_columns<X, Y, NT>(r, dy, x, mean_in, rstd_in, dweight, dbias);
     __shared__ float slots[2][2][NT / kWave];
-    __shared__ float merge[PER > 1 ? 2 * NT * K * V : 1];
     const int l = threadIdx.x % L, group = threadIdx.x / L;
-    const uint32_t stride = gridDim.x * PER, first = blockIdx.x * PER + group;
-    const uint32_t lead = blockIdx.x * PER + (L <= kWave ? threadIdx.x / kWave * (kWave / L) : 0);
+    const uint32_t block = COLUMNS ? blockIdx.x - column_blocks : blockIdx.x, stride = (COLUMNS ? gridDim.x - column_blocks : gridDim.x) * PER, first = block * PER + group;
+    const uint32_t lead = block * PER + (L <= kWave ? threadIdx.x / kWave * (kWave / L) : 0);
     const RowPart<L, K, V> part(l, r.width);
     float w[K][V], dw[K][V], db[K][V];
 #pragma unroll
@@ -178,7 +234,7 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(R
             for (int i = 0; i < V; ++i) {
                 xh[k][i] = (raw_x[k].get(i) - mean) * rstd;
                 g[k][i] = raw_dy[k].get(i);
-                if (there) {   // (of a chunk's values that another one holds too, the other one's sums are written)
+                if (!COLUMNS && there) {   // (of a chunk's values that another one holds too, the other one's sums are written)
                     dw[k][i] += g[k][i] * xh[k][i];
                     db[k][i] += g[k][i];
                 }
@@ -218,7 +274,8 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(R
             }
         }
     }
-    if (!dweight && !dbias) return;
+    if (COLUMNS || (!dweight && !dbias)) return;
+    __shared__ float merge[PER > 1 && !COLUMNS ? 2 * NT * K * V : 1];
     if (PER > 1 && r.groups <= PER) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
@@ -314,16 +371,16 @@ inline unsigned blocks_for(size_t rows, int per, int groups, unsigned most) {
     return (unsigned)(blocks < want ? blocks : want);
 }
 
+// Up to so many rows for every row of the weights, dweight and dbias come from the same launch, which reads x and dy twice: 64 rows of 768 values in bf16 5.5 us and, from partial sums, 9.0; 512 of 768 5.7
+// and 9.1; 512 of 2048 7.8 and 9.3; 256 x 16 heads of 256 6.4 and 18.6; but 1024 of 1024 in float32 14.2 and 8.2.
+constexpr size_t kColumnsRows = 512, kMostBlocks = 65536;
 // launch of the gradient with rows in registers; blocks = 0: none
-// Up to so many rows per group one workgroup does it all and writes dweight and dbias itself, a launch less: 60 rows of 72 values, two a group, 5.5 us and 9.0; 22 of 920, three a group, 7.8 and
-// 8.6; 200 of 72, seven a group, 9.4 and 9.0.
-constexpr uint32_t kAloneRounds = 4;
 struct GradPlan {
     unsigned blocks;
     size_t sum_rows;   // rows of partial sums
 };
 inline GradPlan grad_plan(const Rows& r, int per, int threads) {
-    GradPlan p{r.count <= kAloneRounds * per && per % r.groups == 0 ? 1 : blocks_for(r.count, per, r.groups, kMostGradThreads / threads), 0};
+    GradPlan p{blocks_for(r.count, per, r.groups, kMostGradThreads / threads), 0};
     if (r.groups > per) {   // whole strips: workgroups beyond the rows write zeros
         const size_t unit = lcm_of(r.groups, per) / per;
         p.blocks = unit > (1u << 20) ? 0 : (unsigned)((p.blocks + unit - 1) / unit * unit);
@@ -503,11 +560,21 @@ int flashrnn_layer_norm_bwd(const flashrnn_layer_norm_desc_t* d, const void* dy,
         using X = std::remove_pointer_t<decltype(xt)>;
         using Y = std::remove_pointer_t<decltype(yt)>;
         constexpr int L = decltype(s)::L, K = decltype(s)::K, NT = threads_of<L>();
+        const size_t column_blocks = d->groups * (((size_t)d->width + kSumColumns - 1) / kSumColumns);
+        if (params && tokens <= kColumnsRows && rows <= kMostBlocks && column_blocks <= kMostBlocks) {
+            taken = true;
+            strips = 1;
+            hipLaunchKernelGGL((layer_norm_grad_rows_kernel<X, Y, decltype(v)::value, L, K, true>), dim3((unsigned)(column_blocks + (rows + NT / L - 1) / (NT / L))), dim3(NT), 0, stream,
+                               (uint32_t)column_blocks, r, (const Y*)dy, (const X*)x, weight, d->param_dtype == FLASHRNN_BF16, (const float*)mean, (const float*)rstd, dx,
+                               d->dx_dtype == FLASHRNN_BF16, rows * d->width * type_size(d->dx_dtype) > kStreamBytes, (float*)dweight, (float*)dbias);
+            rc = launch_status();
+            return;
+        }
         const GradPlan p = grad_plan(r, NT / L, NT);
         if (!p.blocks) return;
         taken = true;
         strips = (int)(p.sum_rows / r.groups);
-        hipLaunchKernelGGL((layer_norm_grad_rows_kernel<X, Y, decltype(v)::value, L, K>), dim3(p.blocks), dim3(NT), 0, stream, r, (const Y*)dy, (const X*)x, weight,
+        hipLaunchKernelGGL((layer_norm_grad_rows_kernel<X, Y, decltype(v)::value, L, K, false>), dim3(p.blocks), dim3(NT), 0, stream, 0u, r, (const Y*)dy, (const X*)x, weight,
                            d->param_dtype == FLASHRNN_BF16, (const float*)mean, (const float*)rstd, dx, d->dx_dtype == FLASHRNN_BF16,
                            rows * d->width * type_size(d->dx_dtype) > kStreamBytes, strips == 1 ? (float*)dweight : params ? (float*)workspace : nullptr,
                            strips == 1 ? (float*)dbias : params ? (float*)workspace + p.sum_rows * d->width : nullptr);

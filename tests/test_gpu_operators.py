@@ -212,6 +212,16 @@ def test_layer_norm_of_few_and_many_rows(rows, width):
     _check_norm(_rows(gen, rows, width, BF16), (1 + 0.2 * torch.randn(width, generator=gen)).cuda(), _normal(gen, width), BF16, BF16, gen)
 
 
+@pytest.mark.parametrize("rows", [512, 513, 700])
+@pytest.mark.parametrize("shape", [(9,), (40,), (100,), (260,), (520,), (1001,), (1500,), (2100,), (5000,), (9000,), (12001,), (5, 48), (3, 80), (257, 16), (16, 256)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layer_norm_gradient_on_both_sides_of_one_launch(rows, shape, dtype):
+    """dweight and dbias of few rows are added up beside dx, those of more from partial sums."""
+    gen = _gen(rows + shape[0])
+    wide = _normal(gen, rows, 2, *shape, dtype=dtype)
+    _check_norm(wide[:, 1], (1 + 0.2 * torch.randn(*shape, generator=gen)).to(dtype).cuda(), _normal(gen, *shape, dtype=dtype), dtype, dtype, gen)
+
+
 @pytest.mark.parametrize("x_dtype,dtype,dx_dtype,param_dtype", itertools.product(TYPES, TYPES, TYPES, TYPES))
 @pytest.mark.parametrize("width", [96, 1111])
 def test_layer_norm_of_every_mix_of_types(x_dtype, dtype, dx_dtype, param_dtype, width):
