@@ -268,7 +268,7 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* desc, const void* to
  * Gradient:  g = dy weight,  xh = (x - mean) rstd,  dx = rstd (g - E g - xh E(g xh)),  dweight = sum_rows dy xh,  dbias = sum_rows dy, the
  * two sums in an order that the shape alone decides.
  *   dy       [rows,width] io_dtype
- *   dx       [rows,width] dx_dtype  OUT (dense)
+ *   dx       [rows,width] dx_dtype  OUT (dense; may be dy, or a dense x, of the same type: any other overlap is undefined)
  *   dweight, dbias  [groups,width] f32  OUT, each may be NULL
  *   workspace  flashrnn_layer_norm_workspace_bytes() bytes, 256-byte aligned, any content (may be NULL where both sums are)
  */

@@ -575,7 +575,7 @@ def flashrnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, dtype=None, sav
 
 def flashrnn_layer_norm_bwd(dy, x, mean, rstd, weight=None, dtype=None, param_grads=True, out=None, workspace=None, stream=None):
     """Gradient of flashrnn_layer_norm_fwd.  Returns (dx, dweight, dbias): dx dense, in dy's type or in `dtype`; the others f32 in weight's shape ([D] without a weight), or None
-    where param_grads is false.  `out` may pass preallocated (dx, dweight, dbias)."""
+    where param_grads is false.  `out` may pass preallocated (dx, dweight, dbias); dx may be dy, or a dense x, of its own type."""
     if stream is not None:   # (what is allocated here belongs to that stream, too)
         with torch.cuda.stream(stream):
             return flashrnn_layer_norm_bwd(dy, x, mean, rstd, weight, dtype, param_grads, out, workspace)

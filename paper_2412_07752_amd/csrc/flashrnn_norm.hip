@@ -561,7 +561,7 @@ int flashrnn_layer_norm_bwd(const flashrnn_layer_norm_desc_t* d, const void* dy,
         using Y = std::remove_pointer_t<decltype(yt)>;
         constexpr int L = decltype(s)::L, K = decltype(s)::K, NT = threads_of<L>();
         const size_t column_blocks = d->groups * (((size_t)d->width + kSumColumns - 1) / kSumColumns);
-        if (params && tokens <= kColumnsRows && rows <= kMostBlocks && column_blocks <= kMostBlocks) {
+        if (params && dx != dy && dx != x && tokens <= kColumnsRows && rows <= kMostBlocks && column_blocks <= kMostBlocks) {   // (in place nothing can be read twice)
             taken = true;
             strips = 1;
             hipLaunchKernelGGL((layer_norm_grad_rows_kernel<X, Y, decltype(v)::value, L, K, true>), dim3((unsigned)(column_blocks + (rows + NT / L - 1) / (NT / L))), dim3(NT), 0, stream,

@@ -268,6 +268,23 @@ def test_layer_norm_of_strided_inputs(view):
     _check_norm(x, _normal(gen, 72), _normal(gen, 72), F32, F32, gen)
 
 
+@pytest.mark.parametrize("rows,width", [(1, 8), (40, 100), (40, 3000), (512, 768), (700, 768), (600, 9000), (5, 30000)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layer_norm_gradient_in_place(rows, width, dtype):
+    """dx in dy's or in x's memory: the same bits, dweight and dbias too where the sums run in the same order."""
+    gen = _gen(rows)
+    x, dy, w = _rows(gen, rows, width, dtype), _normal(gen, rows, width, dtype=dtype), _normal(gen, width)
+    _, mean, rstd = api.flashrnn_layer_norm_fwd(x, w)
+    want = api.flashrnn_layer_norm_bwd(dy, x, mean, rstd, w)
+    _, (_, wbound, bbound) = ou.layer_norm_grad(dy, x, mean, rstd, w)
+    for own in range(2):
+        a, b = dy.clone(), x.clone()
+        dx, dw, db = api.flashrnn_layer_norm_bwd(a, b, mean, rstd, w, out=((b, a)[own], torch.empty_like(w), torch.empty_like(w)))
+        assert torch.equal(dx, want[0])
+        ou.check(dw, want[1], 2 * wbound, "dweight")
+        ou.check(db, want[2], 2 * bbound, "dbias")
+
+
 def test_layer_norm_of_no_rows():
     w, b = torch.ones(24, device="cuda"), torch.ones(24, device="cuda")
     x = torch.empty(0, 3, 24, device="cuda")
