@@ -1,7 +1,7 @@
 // Embedding lookup and its gradient by sorted tokens (include/flashrnn.h).
 //
 // out_i = s E[tok_i];  dE[v] = s sum over the places i of v of dout_i, every sum in float32 and in the order of the places, so that no result hangs on which workgroup comes first.  Both are bound by
-// memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 158 us (4.3 TB/s: a sort of four launches takes 27 us of it, the sums
+// memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 157 us (4.3 TB/s: a sort of four launches takes 27 us of it, the sums
 // and the zeros beside them 123, the pieces 8), 4096 places x 768 columns into 32000 words 25.9 us, 32 places of 64 columns 4.9 us.
 //
 // The gradient of up to kFewPlaces places is one launch.  Beyond, it sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs,
