@@ -4,7 +4,7 @@
 // memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 157 us (4.3 TB/s: a sort of four launches takes 27 us of it, the sums
 // and the zeros beside them 123, the pieces 8), 4096 places x 768 columns into 32000 words 25.9 us, 32 places of 64 columns 4.9 us.
 //
-// The gradient of up to kFewPlaces places is one launch.  Beyond, it sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs,
+// The gradient of few places (at most kFewPlaces) is one launch.  Beyond, it sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs,
 // beyond by a radix sort, least significant digit first, of tiles of places.  The table's rows are filled with zeros by the workgroups that the sort leaves idle.  Then groups of lanes
 // add up runs of consecutive sorted places and write the rows of the words that begin and end inside; what is left of a word at the ends of a run goes to the workspace, and a last kernel joins such pieces
 // in order.  Tokens outside the vocabulary sort behind all words.
@@ -512,13 +512,13 @@ __global__ __launch_bounds__(kThreads) void join_pieces_kernel(Sum q, uint32_t r
     put(word, s);
 }
 
-// Up to kFewPlaces places, one launch: a workgroup per place (and one of `spread` parts of the column blocks) looks for the places of its word and, where none comes before its own, adds them up: each
-// group of L lanes a part of them, in order, and the parts in order.  The workgroups beyond fill, with the words in their registers.  Every workgroup reads all tokens, so there are up to kFewBlocks
-// of them, with up to two column blocks each, and no more columns than that: 32 places of 64 columns 4.9 us, by sorting 9.0; 1024 of 768 columns among 300 words 8.1 and 11.7; 512 of 4096 columns
-// 8.9 and 11.6 (without the limit 1024 of 4096 columns 16.5 and 13.8).
-constexpr uint32_t kFewPlaces = 1024, kFewBlocks = 4096;
+// Up to kFewPlaces places, one launch: a workgroup per place (and L * kColumns columns) looks for the places of its word and, where none comes before its own, adds them up: each group of L lanes a part
+// of them, in order, and the parts in order.  The workgroups beyond fill, with the words in their registers.  Every workgroup reads all tokens, so there are up to kFewBlocks of them (1024 places of 4096
+// columns 29 us, by sorting 13.8); and all places may have one word, so a group gets up to kFewRows of them.  Half of the places one word's, the others among 300 words: 256 of 768 columns 5.8 us and,
+// by sorting, 11.3; 512 8.5 and 11.3 (all one word's: 13.7 and 11.3); 1024 13.6 and 11.4 (23.8 and 12.5); 1024 of 64 columns 6.4 and 11.3 (9.2 and 11.1).
+constexpr uint32_t kFewPlaces = 1024, kFewBlocks = 4096, kFewRows = 128;
 template <typename O, int L, bool NARROW, bool ACCUMULATE>
-__global__ __launch_bounds__(kThreads) void few_places_kernel(Sum q, const void* tokens, bool index64, uint32_t spread, Fill fill) {
+__global__ __launch_bounds__(kThreads) void few_places_kernel(Sum q, const void* tokens, bool index64, Fill fill) {
     constexpr int V = kColumns, kGroups = kThreads / L, kAhead = 8, kWaves = kThreads / kWave, kParts = kFewPlaces / kWave;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     if (blockIdx.x >= q.blocks) {
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(kThreads) void few_places_kernel(Sum q, const void*
     __shared__ uint64_t masks[kParts];
     __shared__ uint32_t places[kFewPlaces];
     __shared__ float lds[kGroups][L][V];
-    const uint32_t own = blockIdx.x / spread, word = key_of(tokens, index64, own, q.vocab);
+    const uint32_t own = blockIdx.x / q.column_blocks, word = key_of(tokens, index64, own, q.vocab);
     if (word == q.vocab) return;
     uint64_t mask[kParts / kWaves];   // places of the word, 64 at a time; the wave's
 #pragma unroll
@@ -570,31 +570,28 @@ __global__ __launch_bounds__(kThreads) void few_places_kernel(Sum q, const void*
     __syncthreads();
     const int l = threadIdx.x % L;
     const uint32_t group = threadIdx.x / L, part = (total + kGroups - 1) / kGroups, end = (group + 1) * part < total ? (group + 1) * part : total;
-    for (uint32_t block = blockIdx.x - own * spread; block < q.column_blocks; block += spread) {
-        const Columns<V, NARROW> col(block * L + l, q.width);
-        float s[V] = {};
-        for (uint32_t k = group * part; k < end; k += kAhead) {
-            Chunk<O, V> rows[kAhead];
+    const Columns<V, NARROW> col((blockIdx.x - own * q.column_blocks) * L + l, q.width);
+    float s[V] = {};
+    for (uint32_t k = group * part; k < end; k += kAhead) {
+        Chunk<O, V> rows[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) rows[u] = col.load((const O*)q.dout + (size_t)places[k + u < end ? k + u : end - 1] * q.width);
+        for (int u = 0; u < kAhead; ++u) rows[u] = col.load((const O*)q.dout + (size_t)places[k + u < end ? k + u : end - 1] * q.width);
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (k + u < end)
+        for (int u = 0; u < kAhead; ++u)
+            if (k + u < end)
 #pragma unroll
-                    for (int c = 0; c < V; ++c) s[c] += rows[u].get(c);
-        }
-        if (total > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int c = 0; c < V; ++c) lds[group][l][c] = s[c];
-            __syncthreads();
-        }
-        if (group) continue;
-        for (uint32_t v = 1; v * part < total; ++v)
-#pragma unroll
-            for (int c = 0; c < V; ++c) s[c] += lds[v][l][c];
-        put_row<ACCUMULATE>(q, col, word, nullptr, s);
+                for (int c = 0; c < V; ++c) s[c] += rows[u].get(c);
     }
+    if (total > 1) {
+#pragma unroll
+        for (int c = 0; c < V; ++c) lds[group][l][c] = s[c];
+        __syncthreads();
+    }
+    if (group) return;
+    for (uint32_t v = 1; v * part < total; ++v)
+#pragma unroll
+        for (int c = 0; c < V; ++c) s[c] += lds[v][l][c];
+    put_row<ACCUMULATE>(q, col, word, nullptr, s);
 }
 
 int check_desc(const flashrnn_embedding_desc_t* d, bool gradient) {
@@ -725,15 +722,15 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* d, const void* token
         else launch(Int<8>{}, Int<0>{});
         return launch_status();
     };
-    if (n <= kFewPlaces && n * p.column_blocks <= 2 * kFewBlocks) {
-        const unsigned fills = fill_to(vocab, kThreads / kWave), each = n * p.column_blocks > kFewBlocks ? 2 : 1, spread = (p.column_blocks + each - 1) / each, blocks = (unsigned)n * spread;
+    if (n <= kFewPlaces && n * p.column_blocks <= kFewBlocks && n * p.L <= kFewRows * kThreads) {
+        const unsigned fills = fill_to(vocab, kThreads / kWave), blocks = (unsigned)n * p.column_blocks;
         if (blocks + fills == 0) return FLASHRNN_OK;
         const Sum q{nullptr, nullptr, dout, (float*)dtable, nullptr, (uint32_t)n, vocab, 0, d->width, accumulate, d->scale, (uint32_t)p.column_blocks, blocks};
         return with_io_type(d->io_dtype, [&](auto* ot) {
             using O = std::remove_pointer_t<decltype(ot)>;
             return by_lanes([&](auto lanes, auto narrow) {
                 auto kernel = accumulate ? few_places_kernel<O, decltype(lanes)::value, decltype(narrow)::value, true> : few_places_kernel<O, decltype(lanes)::value, decltype(narrow)::value, false>;
-                hipLaunchKernelGGL(kernel, dim3(blocks + fills), dim3(kThreads), 0, stream, q, tokens, d->index_dtype == FLASHRNN_I64, spread, fill);
+                hipLaunchKernelGGL(kernel, dim3(blocks + fills), dim3(kThreads), 0, stream, q, tokens, d->index_dtype == FLASHRNN_I64, fill);
             });
         });
     }

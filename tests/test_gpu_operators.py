@@ -121,6 +121,12 @@ def test_embedding_gradient_of_few_places(n, vocab, width, dtype, index):
         ou.check(again, 2 * want, 2 * bound + 2 * ou.U * want.abs(), "accumulated")
 
 
+@pytest.mark.parametrize("n,vocab,width", [(512, 300, 768), (513, 300, 768), (256, 9, 4096), (257, 9, 4096), (1024, 33, 128), (1024, 33, 129)])
+@pytest.mark.parametrize("dtype,index", [(F32, torch.int64), (BF16, torch.int32)])
+def test_embedding_gradient_of_the_most_places_that_one_launch_takes(n, vocab, width, dtype, index):
+    test_embedding_gradient_of_few_places(n, vocab, width, dtype, index)
+
+
 def test_embedding_of_places_beyond_32_bit_offsets():
     n, width = (1 << 31) // 4096 + 5000, 4096
     tokens = torch.zeros(n, dtype=torch.int32, device="cuda")
