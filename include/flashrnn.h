@@ -287,6 +287,7 @@ int flashrnn_layer_norm_bwd(const flashrnn_layer_norm_desc_t* desc, const void* 
 /*
  * Cross entropy of rows of logits against one class each, and its gradient in the same pass:
  *     lse = log sum_j exp x_j,   loss = lse - x_target,   dx_j = grad_scale * dloss * (exp(x_j - lse) - [j = target])
+ * Loss and gradient are formed from differences to the row's largest logit: an offset that all logits of a row share costs them no digits.
  * A target outside [0, classes) is ignored: its loss is 0 and so is its row of the gradient.  Classes whose logit is -inf take no part; a row of
  * nothing else has loss +inf and gradient 0.
  *   logits   [rows,classes] io_dtype, rows logits_stride elements apart

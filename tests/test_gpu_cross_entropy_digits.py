@@ -1,0 +1,48 @@
+"""What cross entropy keeps of a row's digits, against 64 bits: the loss whatever offset all logits of the row share."""
+import pytest
+import torch
+
+from operator_util import U, check
+from paper_2412_07752_amd import api
+
+pytestmark = pytest.mark.gpu
+
+CLASSES = [3, 7, 100, 2048, 9000, 70_000, 150_001]   # rows of one value a lane, in the registers of a few lanes to a workgroup, and read twice
+
+
+def chain(classes):
+    """Roundings one behind the other in a row's sum: a thread's values (at most 32 up to 16384 classes, then those that 1024 threads leave each, whole chunks of 8 at the ends), lanes, waves; and where a
+    row is read twice, three for each of a thread's chunks of 4 at which its maximum may rise (what the exponents lose there is part of |d|)."""
+    return max(32, classes // 1024 + 16) + 6 + 16 + (3 * (classes // 4096 + 2) if classes > 65536 else 0)
+
+
+def loss_and_bound(x, t):
+    """(loss, bound).  loss = log s + (top - x_t), s = sum e_j, e_j = exp(d_j), d_j = x_j - top.  The difference is off by U |d|, the product with log2 e and that constant by as much each, the
+    exponential by 2 U: e_j by (2 + 3 |d_j|) U, relative; s by chain U more, which is what log s is off by, beside 4 U of itself (two units in the last place).  Then U of the target's difference and of the sum."""
+    x = x.double()
+    top = x.max(1, keepdim=True).values
+    d = x - top
+    e = torch.exp(d)
+    s = e.sum(1, keepdim=True)
+    far = (e / s * d.abs()).sum(1)
+    down = -d.gather(1, t[:, None])[:, 0]
+    loss = torch.log(s[:, 0]) + down
+    return loss, U * (chain(x.shape[1]) + 2 + 3 * far + 4 * torch.log(s[:, 0]) + down + loss)
+
+
+@pytest.mark.parametrize("classes", CLASSES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_loss_does_not_lose_digits_to_the_offset_of_a_row(classes, dtype):
+    gen = torch.Generator().manual_seed(classes)
+    offsets = torch.tensor([0.0, 100.0, -100.0, 1000.0, -30_000.0, 30_000.0, 1e6, 0.0])
+    x = torch.randn(len(offsets), classes, generator=gen) + offsets[:, None]
+    t = torch.randint(classes, (len(offsets),), generator=gen)
+    t[0], t[1] = classes - 1, 0
+    x[torch.arange(len(offsets)), t] += torch.log(torch.tensor(float(classes))) + 6   # (a target that has nearly all of the probability)
+    x = x.to(dtype).cuda()
+    t = t.cuda()
+    want, bound = loss_and_bound(x, t)
+    loss, _ = api.flashrnn_cross_entropy(x, t)
+    check(loss, want, bound, "loss")
+    alone, _ = api.flashrnn_cross_entropy(x, t, gradient=False)
+    check(alone, want, bound, "loss alone")
