@@ -3,14 +3,12 @@
 // loss = log s + (top - x_t) and dx_j = f (exp(x_j - top) / s - [j = t]) with top the row's largest logit, s = sum exp(x_j - top), f = grad_scale * dloss; lse = top + log s where it is asked for (the loss
 // does not go through lse, whose last place is that of the row's offset: beside logits of 30000 a loss of 0.0092 came out as 0.0098).  The call is
 // bound by memory: a row is read once and its gradient written once, and in between it stays in registers as it lies in memory (16 bytes of it per word of four registers); the exponentials are
-// formed twice rather than kept.  Sums are float32; the exponential is the hardware's 2^x (1 ulp), behind a difference that is exact or rounded once.  16384 x 50304 in bf16: 537 us, 6.1 TB/s.
+// formed twice rather than kept.  Sums are float32.  16384 x 50304 in bf16: 537 us, 6.1 TB/s.
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;
 
 namespace {
-
-constexpr float kLog2e = 1.44269504088896340736f;
 
 struct Problem {
     const void *logits, *targets;
@@ -24,6 +22,15 @@ struct Problem {
 __device__ __forceinline__ int64_t target_of(const Problem& p, size_t row) { return p.index64 ? ((const int64_t*)p.targets)[row] : ((const int32_t*)p.targets)[row]; }
 // exp(x - top): the difference first, so that no finite logit overflows on the way
 __device__ __forceinline__ float exp_below(float x, float top) { return fast_exp2((x - top) * kLog2e); }
+// f exp(x - top), of the logits' type.  In float32 the rounding of d log2 e = y + (d - y ln 2) log2 e would leave classes 80 below the largest off by 62 units of 2^-24, so e^d = 2^y (1 + d - y ln 2), with ln 2
+// in two parts.  (In the sum the plain form does: what it loses grows with the distance, and terms shrink with its exponential.  16384 x 128 in float32 4.95 us with the plain form in both, 5.18 so, 5.4 with the
+// accurate one in both; 16384 x 32000 689, 697 and 733.)
+constexpr float kLn2Hi = 0.693147182464599609375f, kLn2Lo = -1.904654299957767e-9f;
+template <typename X> __device__ __forceinline__ float times_exp_below(float f, float x, float top) {
+    if constexpr (sizeof(X) == 2) return f * exp_below(x, top);
+    const float d = max_nan(x - top, -110.0f), y = d * kLog2e, p = f * fast_exp2(y);   // (-inf: p = 0)
+    return fmaf(p, fmaf(-y, kLn2Lo, fmaf(-y, kLn2Hi, d)), p);
+}
 
 // Groups of L threads hold a row as K chunks of V values each, laid out as RowPart says.  Up to 7 chunks (57344 classes in bf16) the kernel keeps to 64 registers, so that a CU holds two
 // workgroups of 1024 threads and one's loads and stores run beside the other's arithmetic: 16384 x 50304 in bf16 565 us, with one workgroup 653; eight chunks do not fit.
@@ -82,7 +89,7 @@ __global__ __launch_bounds__(threads_of<L>(), L == 1024 && K <= 7 ? 8 : 1) void 
             const bool holds = counts && hit >= 0 && hit < V;
             float g[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[i] = zero ? 0.f : fs * exp_below(raw[k].get(i), top);
+            for (int i = 0; i < V; ++i) g[i] = zero ? 0.f : times_exp_below<X>(fs, raw[k].get(i), top);
             if (holds) {
                 float x = 0.f;
 #pragma unroll
@@ -150,7 +157,7 @@ __global__ __launch_bounds__(NT) void loss_long_kernel(Problem p) {
         auto grad = [&](float v, int j) {
             const bool hit = counts && j == (int)t;
             if (hit) p.loss[row] = s == 0.f ? __builtin_inff() : log_s + (all - v);
-            return zero ? 0.f : fs * exp_below(v, all) - (hit ? f : 0.f);
+            return zero ? 0.f : times_exp_below<X>(fs, v, all) - (hit ? f : 0.f);
         };
         if (!p.dlogits) {
             if (counts && threadIdx.x == 0) p.loss[row] = s == 0.f ? __builtin_inff() : log_s + (all - load_value(x + t));

@@ -1,8 +1,9 @@
-"""What cross entropy keeps of a row's digits, against 64 bits: the loss whatever offset all logits of the row share."""
+"""What cross entropy keeps of a row's digits, against 64 bits: the loss whatever offset all logits of the row share, the gradient of
+classes far below the largest."""
 import pytest
 import torch
 
-from operator_util import U, check
+from operator_util import U, check, rounding
 from paper_2412_07752_amd import api
 
 pytestmark = pytest.mark.gpu
@@ -46,3 +47,19 @@ def test_the_loss_does_not_lose_digits_to_the_offset_of_a_row(classes, dtype):
     check(loss, want, bound, "loss")
     alone, _ = api.flashrnn_cross_entropy(x, t, gradient=False)
     check(alone, want, bound, "loss alone")
+
+
+@pytest.mark.parametrize("classes", CLASSES)
+def test_float32_gradients_of_classes_far_below_the_largest(classes):
+    """The largest logit is 0 and every other 30 to 80 below: the differences are exact and the sum is 1 but for less than U.  What is left is the exponential (4 U: two units in the last place) and a
+    handful of roundings: the sum, its quotient, the product (2 U each)."""
+    gen = torch.Generator().manual_seed(classes)
+    x = -(30 + 50 * torch.rand(5, classes, generator=gen))
+    top, t = torch.randint(classes, (5,), generator=gen), torch.randint(classes, (5,), generator=gen)
+    t[0] = top[0]
+    x[torch.arange(5), top] = 0.0
+    e = torch.exp(x.double())   # (on the host, from its parts: the library's softmax of float64 rows on the GPU is itself off by 60 units of 2^-24 beyond 1024 classes)
+    p = e / e.sum(1, keepdim=True)
+    want = p.scatter_add(1, t[:, None], torch.full((5, 1), -1.0, dtype=torch.float64))
+    _, grad = api.flashrnn_cross_entropy(x.cuda(), t.cuda())
+    check(grad, want, 10 * U * p + rounding(torch.float32, want), "dlogits")
