@@ -316,7 +316,7 @@ int flashrnn_cross_entropy(const flashrnn_cross_entropy_desc_t* desc, const void
  *               NULL (the norm alone); any other overlap is undefined
  *   sizes       HOST array: values per tensor, >= 0
  *   dtypes      HOST array: flashrnn_dtype_t of grads[k] and out[k]
- *   norm        [1] f32  OUT
+ *   norm        [1] f32  OUT (infinity where it is beyond float32; the factor comes from its value in 64 bits)
  *   workspace   flashrnn_grad_clip_workspace_bytes(count) bytes, 256-byte aligned, any content
  * The host arrays are read before the call returns.
  */
