@@ -673,6 +673,7 @@ def flashrnn_grad_clip(grads, max_norm, out=None, norm=None, workspace=None, str
             raise ValueError("norm is required where there are no gradients")
         norm = torch.empty(1, dtype=torch.float32, device=grads[0].device)
     _chk(norm, (1,), torch.float32, "norm")
+    _same_device(norm, workspace=workspace)
     for i, (g, o) in enumerate(zip(grads, to)):
         _chk(g, g.shape, g.dtype, f"grads[{i}]")
         if o is not g:
