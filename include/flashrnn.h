@@ -263,7 +263,7 @@ int flashrnn_embedding_bwd(const flashrnn_embedding_desc_t* desc, const void* to
  * flashrnn_fwd call are the rows of states + S*B*NH*D with rows_outer = T, rows_inner = B, groups = NH, x_stride = S*B*NH*D.
  *   x        x_dtype, as above
  *   weight, bias  [groups,width] param_dtype, each may be NULL (ones, zeros)
- *   y        [rows,width] io_dtype  OUT
+ *   y        [rows,width] io_dtype  OUT (dense; may be a dense x, of the same type: any other overlap is undefined)
  *   mean, rstd  [rows] f32          OUT, both NULL for a call that saves nothing (rows = rows_outer * rows_inner * groups)
  * Gradient:  g = dy weight,  xh = (x - mean) rstd,  dx = rstd (g - E g - xh E(g xh)),  dweight = sum_rows dy xh,  dbias = sum_rows dy, the
  * two sums in an order that the shape alone decides.

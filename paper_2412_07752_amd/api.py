@@ -545,7 +545,7 @@ def _norm_desc(x, weight, bias, io, dx, eps):
 
 def flashrnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, dtype=None, save_for_backward=True, y=None, mean=None, rstd=None, stream=None):
     """Layer norm over the last axis of x, in x's type or in `dtype`.  weight, bias: [D], or [NH, D] for x[..., NH, D] (head by head), or None.  x may have one leading
-    axis that is not dense, as the hidden states states[1:, 0] of a flashrnn_fwd call.  Returns (y, mean, rstd), the last two f32 of x.shape[:-1], or None, None."""
+    axis that is not dense, as the hidden states states[1:, 0] of a flashrnn_fwd call; y may be a dense x, of its own type.  Returns (y, mean, rstd), the last two f32 of x.shape[:-1], or None, None."""
     if stream is not None:   # (what is allocated here belongs to that stream, too)
         with torch.cuda.stream(stream):
             return flashrnn_layer_norm_fwd(x, weight, bias, eps, dtype, save_for_backward, y, mean, rstd)

@@ -19,6 +19,7 @@ constexpr unsigned kMostThreads = 8192 * 256;
 constexpr unsigned kMostGradThreads = 512 * 256;
 constexpr int kMaxStrips = 256;   // workgroups that add up the gradients of weight and bias, each over a strip of rows
 
+// y may be x, and dx dy or x: a row is read, by the threads that hold it, before anything of it is written, and no pointer of the three is restricted.
 struct Rows {
     long long x_stride;
     uint32_t count, per_outer;   // rows, and those of one outer block
@@ -30,7 +31,7 @@ __device__ __forceinline__ size_t x_offset(const Rows& r, uint32_t row) {
 }
 
 template <typename X, typename Y, typename P>
-__global__ __launch_bounds__(kThreads) void layer_norm_fwd_kernel(Rows r, const X* __restrict__ x, const P* __restrict__ weight, const P* __restrict__ bias, Y* __restrict__ y,
+__global__ __launch_bounds__(kThreads) void layer_norm_fwd_kernel(Rows r, const X* x, const P* __restrict__ weight, const P* __restrict__ bias, Y* y,
                                                                   float* __restrict__ mean_out, float* __restrict__ rstd_out, float eps) {
     __shared__ float lds[kThreads / kWave];
     for (uint32_t row = blockIdx.x; row < r.count; row += gridDim.x) {
@@ -61,8 +62,8 @@ __global__ __launch_bounds__(kThreads) void layer_norm_fwd_kernel(Rows r, const 
 // Rows in registers, laid out as RowPart says, read once.  Groups take rows a fixed number apart, which is a multiple of `groups`, so that a thread's part of weight and bias
 // stays in its registers; the next row's loads are on their way while this row is worked on.
 template <typename X, int V, int L, int K>
-__global__ __launch_bounds__(threads_of<L>()) void layer_norm_rows_kernel(Rows r, const X* __restrict__ x, const void* __restrict__ weight, const void* __restrict__ bias,
-                                                                         bool params_bf16, void* __restrict__ y, bool y_bf16, bool stream, float* __restrict__ mean_out,
+__global__ __launch_bounds__(threads_of<L>()) void layer_norm_rows_kernel(Rows r, const X* x, const void* __restrict__ weight, const void* __restrict__ bias,
+                                                                         bool params_bf16, void* y, bool y_bf16, bool stream, float* __restrict__ mean_out,
                                                                          float* __restrict__ rstd_out, float eps) {
     constexpr int NT = threads_of<L>(), PER = NT / L;   // groups of threads in a workgroup
     __shared__ float slots[2][NT / kWave];
@@ -186,9 +187,9 @@ __device__ __forceinline__ void sum_columns(const Rows& r, const Y* __restrict__
     }
 }
 template <typename X, typename Y, int V, int L, int K, bool COLUMNS>
-__global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(uint32_t column_blocks, Rows r, const Y* __restrict__ dy, const X* __restrict__ x, const void* __restrict__ weight,
+__global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(uint32_t column_blocks, Rows r, const Y* dy, const X* x, const void* __restrict__ weight,
                                                                               bool weight_bf16, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-                                                                              void* __restrict__ dx, bool dx_bf16, bool stream, float* __restrict__ dweight, float* __restrict__ dbias) {
+                                                                              void* dx, bool dx_bf16, bool stream, float* __restrict__ dweight, float* __restrict__ dbias) {
     constexpr int NT = threads_of<L>(), PER = NT / L;
     if (COLUMNS && blockIdx.x < column_blocks) return sum_columns<X, Y, NT>(r, dy, x, mean_in, rstd_in, dweight, dbias);
     __shared__ float slots[2][2][NT / kWave];
@@ -213,13 +214,13 @@ __global__ __launch_bounds__(threads_of<L>()) void layer_norm_grad_rows_kernel(u
         row = row < r.count ? row : r.count - 1;
         const X* p = x + x_offset(r, row);
         const Y* q = dy + (size_t)row * r.width;
+        mean = mean_in[row];   // (ahead of the row: 65536 x 2048 values in bf16 148 us, behind it 154)
+        rstd = rstd_in[row];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             raw_x[k].load(p + part.at[k]);
             raw_dy[k].load(q + part.at[k]);
         }
-        mean = mean_in[row];
-        rstd = rstd_in[row];
     };
     fetch(first);
     const float n = (float)r.width;
@@ -391,8 +392,8 @@ inline GradPlan grad_plan(const Rows& r, int per, int threads) {
 }
 
 template <typename X, typename Y, typename DX, typename P>
-__global__ __launch_bounds__(kThreads) void layer_norm_dx_kernel(Rows r, const Y* __restrict__ dy, const X* __restrict__ x, const P* __restrict__ weight,
-                                                                 const float* __restrict__ mean_in, const float* __restrict__ rstd_in, DX* __restrict__ dx) {
+__global__ __launch_bounds__(kThreads) void layer_norm_dx_kernel(Rows r, const Y* dy, const X* x, const P* __restrict__ weight,
+                                                                 const float* __restrict__ mean_in, const float* __restrict__ rstd_in, DX* dx) {
     __shared__ float lds[kThreads / kWave];
     for (uint32_t row = blockIdx.x; row < r.count; row += gridDim.x) {
         const X* xr = x + x_offset(r, row);
