@@ -106,15 +106,17 @@ class LanguageModel:
         return n.view(B, self.H) @ table.t()
 
     def generate(self, prompt, count):
-        """prompt[T, B] -> the `count` most likely next words, [count, B]."""
-        states, out = self.start(prompt.shape[1]), []
-        for words in prompt:
+        """prompt[T, B] of at least one word -> the `count` most likely next words, [count, B]."""
+        if prompt.shape[0] == 0 or count < 0:
+            raise ValueError(f"a prompt of {prompt.shape[0]} words cannot be continued by {count}")
+        states, out = self.start(prompt.shape[1]), prompt.new_empty((count, prompt.shape[1]), dtype=torch.int64)
+        for words in prompt if count else ():
             logits = self.step(words, states)
-        for _ in range(count):
-            out.append(logits.argmax(1))
-            if len(out) < count:
-                logits = self.step(out[-1], states)
-        return torch.stack(out)
+        for i in range(count):
+            torch.argmax(logits, 1, out=out[i])
+            if i + 1 < count:
+                logits = self.step(out[i], states)
+        return out
 
 
 def chain_text(vocab, length, batch, seed=0, device="cuda"):
