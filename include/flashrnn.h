@@ -238,8 +238,8 @@ typedef enum { FLASHRNN_I32 = 2, FLASHRNN_I64 = 3 } flashrnn_index_t;
  *   table   [vocab,width]  table_dtype
  *   tokens  [tokens]       index_dtype
  *   out     [tokens,width] io_dtype
- * Gradient:  dtable[v] = scale * sum over the places i of word v of dout[i],  each sum in the order of the places (the tokens are sorted
- * first): the result does not depend on how the workgroups run.
+ * Gradient:  dtable[v] = scale * sum over the places i of word v of dout[i],  each sum in an order that the sizes and the tokens decide (parts of
+ * consecutive places of the word, then the parts): the result does not depend on how the workgroups run.
  *   dout    [tokens,width] io_dtype
  *   dtable  [vocab,width]  f32      OUT: every row, zeros for words that do not occur; accumulate != 0: the sums are added to what is there and
  *                                   other rows are not touched (weights tied to an output layer)

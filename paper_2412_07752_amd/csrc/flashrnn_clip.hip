@@ -1,18 +1,19 @@
 // Clipping of many gradient tensors by their global norm (include/flashrnn.h).
 //
 // norm = sqrt(sum g^2), out = g min(1, max_norm / norm).  Bound by memory: two reads, the second behind the norm, and a write.  Tensors of any number and size are cut into chunks that workgroups take in a
-// fixed order; the tensors' places travel as a kernel argument, so that a call keeps nothing and can be captured.  330 M float32 values out of place 708 us: norm 215 us (6.1 TB/s), products 492 us
-// (5.4 TB/s).  A single layer's 49,000 values: 3.5 and 4.6 us, one launch behind the other.
+// fixed order; the tensors' places travel as a kernel argument, so that a call keeps nothing and can be captured.  330 M float32 values out of place 707 us: norm 214 us (6.2 TB/s), products 491 us
+// (5.4 TB/s).  A single layer's 49,000 values: 3.6 and 4.7 us, one launch behind the other.  (All values by one workgroup, in one launch: 5.6 us for 2000 of them, where the two launches, bound by the host,
+// take 7.5 to 9.8; but 9.6 for 49,500 and 19 for 21 tensors.)
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;
 
 namespace {
 
-constexpr int kTensors = 128;      // tensors per launch: their table is a kernel argument, which holds 4 KB
-constexpr int kMaxBlocks = 1024;   // workgroups per launch, each with a partial sum (683 MB of bf16 values 359 us, with 2048 workgroups 377)
+constexpr int kTensors = 128;      // tensors per launch: their table is a kernel argument, which holds 4 KB (with 16 a small call takes as long)
+constexpr int kMaxBlocks = 1024;   // workgroups per launch, each with a partial sum (683 MB of bf16 values 330 us, with 2048 workgroups 364; 1.3 GB of float32 714 and 726)
 constexpr int kMaxCount = 1 << 24;
-constexpr int kChunk = 8192;       // values of one tensor that a workgroup takes at a time
+constexpr int kChunk = 8192;       // values of one tensor that a workgroup takes at a time (32 KB whatever the type, the tensor found by a ballot, the first loads ahead of the norm: 4.4 + 5.7 us a small call, 1.3 GB 755)
 
 struct Table {
     const void* in[kTensors];

@@ -1,13 +1,13 @@
 // Embedding lookup and its gradient by sorted tokens (include/flashrnn.h).
 //
-// out_i = s E[tok_i];  dE[v] = s sum over the places i of v of dout_i, every sum in float32 and in the order of the places, so that no result hangs on which workgroup comes first.  Both are bound by
+// out_i = s E[tok_i];  dE[v] = s sum over the places i of v of dout_i, every sum in float32 and in an order that sizes and tokens alone decide, so that no result hangs on which workgroup comes first.  Both are bound by
 // memory, the gradient of few places by its launches: 65536 places x 2048 columns in bf16 61 us (5.5 TB/s); gradient into 50304 words 157 us (4.3 TB/s: a sort of four launches takes 27 us of it, the sums
 // and the zeros beside them 123, the pieces 8), 4096 places x 768 columns into 32000 words 25.9 us, 32 places of 64 columns 4.9 us.
 //
 // The gradient of few places (at most kFewPlaces) is one launch.  Beyond, it sorts the places by their word, stable, so that the places of a word stay in order: up to kSmall places by counting over all pairs,
 // beyond by a radix sort, least significant digit first, of tiles of places.  The table's rows are filled with zeros by the workgroups that the sort leaves idle.  Then groups of lanes
-// add up runs of consecutive sorted places and write the rows of the words that begin and end inside; what is left of a word at the ends of a run goes to the workspace, and a last kernel joins such pieces
-// in order.  Tokens outside the vocabulary sort behind all words.
+// add up runs of consecutive sorted places and write the rows of the words that begin and end inside; what is left of a word at the ends of a run goes to the workspace, and a last kernel joins such pieces:
+// in order where they are few, by several groups of lanes where a word goes on through kManyRuns runs and more.  Tokens outside the vocabulary sort behind all words.
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;
@@ -16,8 +16,9 @@ namespace {
 
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
-// Places that are sorted by counting, the bits of their numbers, and those that a workgroup ranks.  Whole gradients of 80 columns: 11525 places 24.3 us by counting and 31.7 by tiles,
-// 16000 places 34.2 and 27.0.
+// Places that are sorted by counting, the bits of their numbers, and those that a workgroup ranks.  Whole gradients of 80 columns among 32000 words: 4096 places 12.5 us by counting and 27.3 by tiles, 12288 places
+// 24.8 and 29.2, 15360 places 33.2 and 30.1; of 768 columns 25.9 and 37.7, 40.5 and 42.1, 47.9 and 43.0.  Among 300 words, which tiles sort in one pass, counting is ahead up to some 8192 places
+// (768 columns: 21.5 and 21.9; 12288 places 29.7 and 22.7).
 constexpr int kSmall = 12288, kSmallBits = 14, kRanked = 16;
 // Tiles of a larger sort, each of which adds up the counts of all: 300000 places of 64 columns 49.5 us, with 128 tiles 53.9 and with 512 as with 256; a million 66.3, 68.8, and with 512 90.
 constexpr int kMaxTiles = 256;
@@ -514,7 +515,8 @@ __global__ __launch_bounds__(kThreads) void join_pieces_kernel(Sum q, uint32_t r
 
 // Up to kFewPlaces places, one launch: a workgroup per place (and L * kColumns columns) looks for the places of its word and, where none comes before its own, adds them up: each group of L lanes a part
 // of them, in order, and the parts in order.  The workgroups beyond fill, with the words in their registers.  Every workgroup reads all tokens, so there are up to kFewBlocks of them (1024 places of 4096
-// columns 29 us, by sorting 13.8); and all places may have one word, so a group gets up to kFewRows of them.  Half of the places one word's, the others among 300 words: 256 of 768 columns 5.8 us and,
+// columns 29 us, by sorting 13.8); and all places may have one word, so a group gets up to kFewRows of them (with the loads of 16 or 32 of its rows on their way instead of 8 this is no faster: the wave's own
+// instructions bound it).  Half of the places one word's, the others among 300 words: 256 of 768 columns 5.8 us and,
 // by sorting, 11.3; 512 8.5 and 11.3 (all one word's: 13.7 and 11.3); 1024 13.6 and 11.4 (23.8 and 12.5); 1024 of 64 columns 6.4 and 11.3 (9.2 and 11.1).
 constexpr uint32_t kFewPlaces = 1024, kFewBlocks = 4096, kFewRows = 128;
 template <typename O, int L, bool NARROW, bool ACCUMULATE>
@@ -603,7 +605,8 @@ int check_desc(const flashrnn_embedding_desc_t* d, bool gradient) {
     return FLASHRNN_OK;
 }
 
-// lanes per row: the number that leaves the fewest of them without columns, the larger one of equals
+// lanes per row: the number that leaves the fewest of them without columns, the larger one of equals.  (A width with a small remainder gets few lanes and many blocks of columns, as 1100 does with 8 and 35: fewer
+// of its places go into one launch, up to 117 where 1024 columns allow 512, and 16384 of them among 32000 words take 57.7 us, of 1152 columns 52.8.)
 int lanes_for(int chunks) {
     int best = 64;
     for (int L = 32; L >= 8; L /= 2)

@@ -3,7 +3,7 @@
 // loss = log s + (top - x_t) and dx_j = f (exp(x_j - top) / s - [j = t]) with top the row's largest logit, s = sum exp(x_j - top), f = grad_scale * dloss; lse = top + log s where it is asked for (the loss
 // does not go through lse, whose last place is that of the row's offset: beside logits of 30000 a loss of 0.0092 came out as 0.0098).  The call is
 // bound by memory: a row is read once and its gradient written once, and in between it stays in registers as it lies in memory (16 bytes of it per word of four registers); the exponentials are
-// formed twice rather than kept.  Sums are float32.  16384 x 50304 in bf16: 537 us, 6.1 TB/s.
+// formed twice rather than kept.  Sums are float32.  16384 x 50304 in bf16: 531 us, 6.2 TB/s; the loss alone 386, 4.3 TB/s.
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;

@@ -2,9 +2,9 @@
 //
 // y = (x - mean) rstd w + b;  dx = rstd (g - E g - xh E(g xh)) with g = dy w, xh = (x - mean) rstd;  dw = sum dy xh, db = sum dy.  Both directions are bound by memory: x (and dy) are read once, y (or dx)
 // is written once, and the row stays in registers between its sums; the mean first, then the squares around it, so that an offset costs no digits.  All sums are float32.  Measured:
-// forward 65536 x 8 x 256 float32 states to bf16 141 us (5.7 TB/s), 65536 x 2048 bf16 91 us (5.9 TB/s); gradient 65536 x 8 x 256 197 us (5.5 TB/s), 16384 x 768 bf16 18.7 us (4.0 TB/s, 4 us of it the
-// second kernel), up to 512 rows in one launch: 64 x 768 bf16 5.4 us.  Rows of fewer than 8 values, and of more than 16384 (bf16: 24576) forward or 12288 (all bf16: 16384) backward, take general kernels that read them several times (30000 float32 values: 1.1 TB/s
-// forward; 16000: 1.2 backward).
+// forward 65536 x 8 x 256 float32 states to bf16 141 us (5.7 TB/s), 65536 x 2048 bf16 91 us (5.9 TB/s); gradient 65536 x 8 x 256 199 us (5.4 TB/s), 16384 x 768 bf16 18.9 us (4.0 TB/s, 4 us of it the
+// second kernel), up to 512 rows in one launch: 64 x 768 bf16 5.7 us.  Rows of fewer than 8 values, and of more than 16384 (bf16: 24576) forward or 12288 (all bf16: 16384) backward, take general kernels that read them several times, a value at a time
+// (float32, 3000 x 30000 forward 1.6 TB/s, 20000 rows 1.7; 3000 x 16000 backward 1.6, 20000 rows 2.1).
 #include "flashrnn_rows.h"
 
 using namespace flashrnn;
