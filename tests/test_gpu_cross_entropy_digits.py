@@ -17,18 +17,21 @@ def chain(classes):
     return max(32, classes // 1024 + 16) + 6 + 16 + (3 * (classes // 4096 + 2) if classes > 65536 else 0)
 
 
-def loss_and_bound(x, t):
-    """(loss, bound).  loss = log s + (top - x_t), s = sum e_j, e_j = exp(d_j), d_j = x_j - top.  The difference is off by U |d|, the product with log2 e and that constant by as much each, the
-    exponential by 2 U: e_j by (2 + 3 |d_j|) U, relative; s by chain U more, which is what log s is off by, beside 4 U of itself (two units in the last place).  Then U of the target's difference and of the sum."""
-    x = x.double()
+def sum_and_bound(x):
+    """(top, s, relative bound of s) of float64 rows, for loss_and_bound and the gradient."""
     top = x.max(1, keepdim=True).values
     d = x - top
     e = torch.exp(d)
     s = e.sum(1, keepdim=True)
-    far = (e / s * d.abs()).sum(1)
-    down = -d.gather(1, t[:, None])[:, 0]
-    loss = torch.log(s[:, 0]) + down
-    return loss, U * (chain(x.shape[1]) + 2 + 3 * far + 4 * torch.log(s[:, 0]) + down + loss)
+    return top, s, U * (chain(x.shape[1]) + 2 + 3 * (e / s * d.abs()).sum(1, keepdim=True))
+
+
+def loss_and_bound(x, t):
+    """(loss, bound).  loss = log s + (top - x_t), s = sum e_j, e_j = exp(d_j), d_j = x_j - top.  The difference is off by U |d|, the product with log2 e and that constant by as much each, the
+    exponential by 2 U: e_j by (2 + 3 |d_j|) U, relative; s by chain U more, which is what log s is off by, beside 4 U of itself (two units in the last place).  Then U of the target's difference and of the sum."""
+    top, s, off = sum_and_bound(x.double())
+    log_s, down = torch.log(s)[:, 0], (top - x.double().gather(1, t[:, None]))[:, 0]
+    return log_s + down, off[:, 0] + U * (4 * log_s + 2 * down + log_s)
 
 
 @pytest.mark.parametrize("classes", CLASSES)
@@ -63,3 +66,22 @@ def test_float32_gradients_of_classes_far_below_the_largest(classes):
     want = p.scatter_add(1, t[:, None], torch.full((5, 1), -1.0, dtype=torch.float64))
     _, grad = api.flashrnn_cross_entropy(x.cuda(), t.cuda())
     check(grad, want, 10 * U * p + rounding(torch.float32, want), "dlogits")
+
+
+@pytest.mark.parametrize("classes", [3, 40, 256, 1000, 9000, 65_536, 131_072, 150_001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_and_lse_to_the_bounds_of_a_row_of_their_length(classes, dtype):
+    """p = f e / s: s as loss_and_bound has it, e in the gradient by 4 U (bf16 logits: by (2 + 3 |d|) U), the quotient, the product and the difference by U each."""
+    gen = torch.Generator().manual_seed(classes + 1)
+    x = (torch.randn(7, classes, generator=gen) * 3).to(dtype)
+    t = torch.randint(classes, (7,), generator=gen)
+    top, s, off = sum_and_bound(x.double())
+    d = x.double() - top
+    p = torch.exp(d) / s
+    hot = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
+    bound = p * (off + U * (4 if dtype == torch.float32 else 2 + 3 * d.abs()) + 2 * U) + U * (p - hot).abs() + 2.0 ** -126
+    want_lse = (torch.log(s) + top)[:, 0]
+    lse = torch.empty(7, device="cuda")
+    _, grad = api.flashrnn_cross_entropy(x.cuda(), t.cuda(), lse=lse)
+    check(grad, p - hot, bound + (rounding(dtype, p - hot) if dtype == torch.bfloat16 else 0), "dlogits")
+    check(lse, want_lse, off[:, 0] + U * (4 * torch.log(s)[:, 0] + want_lse.abs()), "lse")
